@@ -442,6 +442,69 @@ int tvmattn_linear_jvp_bwd(int R, int K, int F, int dtype,
                            void* gx, void* gtx, void* gw, void* gbias,
                            void* workspace, size_t workspace_bytes, void* hip_stream);
 
+/*
+ * ---- 8-bit rows.  For a network that is run and not trained (sampling; the target network of the loss): the operands of
+ * the block's linear layers as 8-bit integers with one float32 scale per row.  A row v of C values becomes
+ *
+ *     s = max_j |v_j| / 127,     q_j = v_j 127 / max|v| rounded to the nearest integer (ties to even)
+ *
+ * and stands for q s (|v_j - q_j s| <= s (1/2 + 2^-16)).  A row with nothing above 2^-100 has s = 0 and q = 0; a row that holds a
+ * NaN or an infinity has s = NaN and q = 0: all that is made of it is NaN, and no other row is touched.
+ * Every operator carries an optional tangent: its rows are rows like any others, with scales of their own.  Without one, the
+ * tangent's pointers (inputs and outputs) are all NULL; some of them alone NULL is TVMATTN_INVALID_ARG.
+ * q, tq: int8, dense.  s, ts: float32, one per row, 4-byte aligned.  There is no backward: rounding has no derivative.
+ *
+ * Rows as they are: a weight (its rows are the output channels), or the attention's output.
+ *   in : x, tx   R rows of C elements of `dtype`, ldx elements apart (0 = C: dense)
+ *   out: q, tq   [R,C] int8;  s, ts [R] float32
+ * C and ldx must be whole numbers of 16-byte chunks, C at most 4096 of them; otherwise TVMATTN_UNSUPPORTED.  One launch.
+ */
+int tvmattn_rowquant_fwd(int R, int C, int dtype, const void* x, const void* tx, long long ldx,
+                         void* q, float* s, void* tq, float* ts, void* hip_stream);
+
+/*
+ * The MLP's activation (tvmattn_gelu_jvp_fwd: a = gelu(u), ta = gelu'(u) tu) with its outputs as 8-bit rows; a and ta are not
+ * rounded in between.  Arguments and limits as above.
+ */
+int tvmattn_gelu_jvp_fwd_q8(int R, int C, int dtype, const void* u, const void* tu, long long ldu,
+                            void* q, float* s, void* tq, float* ts, void* hip_stream);
+
+/*
+ * The gated residual and the modulation behind it (tvmattn_gate_jvp_fwd, then tvmattn_adaln_jvp_fwd on its result), with the
+ * modulated tokens as 8-bit rows:
+ *
+ *     z = x + RMSNorm^-(c) o h,     y = RMSNorm^-(z) o RMSNorm^-(a) + RMSNorm^-(b)     -> z, and y in 8 bits
+ *
+ *   in : x, tx, h, th            [B,T,C] dtype, contiguous;  c, tc, a, ta, b, tb [B,C] float32, contiguous;  eps >= 0, finite
+ *   out: z, tz                   [B,T,C] dtype, rounded once (the modulation takes them unrounded); z may be x itself and tz may be
+ *                                tx itself
+ *        q, tq [B*T,C] int8;  s, ts [B*T] float32
+ * h NULL: no residual; c, th, tc, z and tz are NULL too, and y is the modulation of x (a block's entry).
+ * C must be a multiple of 16 bytes' worth of elements and at most 512 such chunks, B at most 65535; otherwise
+ * TVMATTN_UNSUPPORTED.  One launch, no workspace.  Arithmetic is float32.
+ */
+int tvmattn_gate_adaln_jvp_fwd_q8(int B, int T, int C, int dtype,
+                                  const void* x, const void* tx, const void* h, const void* th,
+                                  const float* c, const float* tc, const float* a, const float* ta,
+                                  const float* b, const float* tb, float eps,
+                                  void* z, void* tz, void* q, float* s, void* tq, float* ts, void* hip_stream);
+
+/*
+ * A linear layer (tvmattn_linear_jvp_fwd) on 8-bit rows and an 8-bit weight:
+ *
+ *     y_rf = (sum_k xq_rk wq_fk) xs_r ws_f + bias_f,     ty_rf = (sum_k txq_rk wq_fk) txs_r ws_f
+ *
+ *   in : xq, txq   R rows of K int8, ldx apart (0 = K: dense);  xs, txs [R] float32
+ *        wq        [F,K] int8, contiguous;  ws [F] float32, 16-byte aligned
+ *        bias      [F] dtype, or NULL
+ *   out: y, ty     [R,F] dtype (float32 or bfloat16), rows ldy elements apart (0 = F: dense)
+ * The sums are exact (32-bit integers); they are scaled in float32 and rounded once.  K and ldx must be multiples of 16, F and
+ * ldy of 8, K at most 2^16, F and the pitches at most 2^20; otherwise TVMATTN_UNSUPPORTED.  One launch, no workspace.
+ */
+int tvmattn_linear_jvp_fwd_q8(int R, int K, int F, int dtype, const void* xq, const float* xs, const void* txq,
+                              const float* txs, long long ldx, const void* wq, const float* ws, const void* bias,
+                              void* y, void* ty, long long ldy, void* hip_stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -10,4 +10,5 @@ from .binding import (TvmattnError, tvmattn_adaln_jvp_bwd, tvmattn_adaln_jvp_fwd
                       tvmattn_qknorm_jvp_fwd, tvmattn_jvp_fwd_qknorm, tvmattn_strerror, tvmattn_jvp_bwd_static, tvmattn_linear_jvp_fwd, tvmattn_linear_jvp_bwd,
                       tvmattn_linear_jvp_bwd_workspace_bytes, TVMATTN_FLAG_PLAIN_ALU,
                       TVMATTN_STATIC_MAX_ROWS,
+                      tvmattn_gate_adaln_jvp_fwd_q8, tvmattn_gelu_jvp_fwd_q8, tvmattn_linear_jvp_fwd_q8, tvmattn_rowquant_fwd,
                       tvmattn_version)

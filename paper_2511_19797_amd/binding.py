@@ -100,6 +100,13 @@ def lib():
         L.tvmattn_linear_jvp_fwd.argtypes = [_I] * 4 + [_P, _P, _LL, _P, _P, _P, _P, _LL, _P]
         L.tvmattn_linear_jvp_bwd.restype = ctypes.c_int
         L.tvmattn_linear_jvp_bwd.argtypes = [_I] * 4 + [_P, _P, _LL, _P, _P, _P, _LL] + [_P] * 5 + [ctypes.c_size_t, _P]
+        for name in ("rowquant_fwd", "gelu_jvp_fwd_q8"):
+            entry = getattr(L, "tvmattn_" + name)
+            entry.restype, entry.argtypes = ctypes.c_int, [_I] * 3 + [_P, _P, _LL] + [_P] * 5
+        L.tvmattn_gate_adaln_jvp_fwd_q8.restype = ctypes.c_int
+        L.tvmattn_gate_adaln_jvp_fwd_q8.argtypes = [_I] * 4 + [_P] * 10 + [ctypes.c_float] + [_P] * 7
+        L.tvmattn_linear_jvp_fwd_q8.restype = ctypes.c_int
+        L.tvmattn_linear_jvp_fwd_q8.argtypes = [_I] * 4 + [_P] * 4 + [_LL] + [_P] * 5 + [_LL, _P]
         _lib = L
     return _lib
 
@@ -622,3 +629,153 @@ def tvmattn_linear_jvp_bwd(x, tx, w, gy, gty, bias_grad=True, out=None, workspac
                                         gty.data_ptr(), ldy, gx.data_ptr(), gtx.data_ptr(), gw.data_ptr(), _ptr(gb),
                                         workspace.data_ptr(), workspace.numel() * workspace.element_size(), _stream()))
     return out
+
+
+# ---- 8-bit rows: int8 values and one float32 scale per row (include/tvmattn.h); a tangent is optional throughout
+def _here(t):
+    """The library launches on the current device, on its current stream."""
+    if t.device.index != torch.cuda.current_device():
+        raise ValueError(f"tensors are on {t.device}, the current device is {torch.cuda.current_device()}")
+
+
+def _pitched(t, cols, what):
+    R, ld = _rows(t, cols, what)
+    if ld < cols:
+        raise ValueError(f"{what}: rows overlap")
+    _here(t)
+    return R, ld
+
+
+def _dtype_of(t):
+    dt = TVMATTN_F32 if t.dtype == torch.float32 else TVMATTN_BF16 if t.dtype == torch.bfloat16 else None
+    if dt is None:
+        raise ValueError(f"unsupported dtype {t.dtype}")
+    return dt
+
+
+def _rows8_out(shape, device, tangent, out):
+    """(q, s, tq, ts) for rows of `shape`, new or checked."""
+    kinds = ((shape, torch.int8), (shape[:-1], torch.float32)) * 2
+    if out is None:
+        return tuple(torch.empty(sh, dtype=dt, device=device) if n < 2 or tangent else None for n, (sh, dt) in enumerate(kinds))
+    out = tuple(out)
+    if len(out) != 4 or (out[2] is None) == tangent or (out[3] is None) == tangent:
+        raise ValueError("out must be (q, s, tq, ts), the last two None without a tangent")
+    for t, (sh, dt) in zip(out, kinds):
+        if t is not None and (t.shape != sh or t.dtype != dt or not t.is_contiguous() or t.device != device):
+            raise ValueError("outputs must be contiguous int8 [..., C] and float32 [...] tensors on the inputs' device")
+    return out
+
+
+def _rows8_call(entry, x, tx, out):
+    if x.dim() < 1:
+        raise ValueError("expected rows")
+    R, ld = _pitched(x, x.shape[-1], "x")
+    dt = _dtype_of(x)
+    if tx is not None and (tx.shape != x.shape or tx.dtype != x.dtype or tx.stride() != x.stride() or tx.device != x.device):
+        raise ValueError("rows and their tangent must agree in shape, dtype and layout")
+    q, s, tq, ts = out = _rows8_out(x.shape, x.device, tx is not None, out)
+    _check(entry(R, x.shape[-1], dt, x.data_ptr(), _ptr(tx), ld, q.data_ptr(), s.data_ptr(), _ptr(tq), _ptr(ts), _stream()))
+    return out
+
+
+def tvmattn_rowquant_fwd(x, tx=None, out=None):
+    """Returns (q, s, tq, ts): the rows of x and tx ([..., C], or 2-D [R, C] views with a row pitch) as int8 [..., C] and float32
+    scales [...]; q s stands for x.  tq and ts are None without tx."""
+    if out is None:
+        r = (_fast or _load_fast()).rowquant(x, tx)
+        if r is not None:
+            return _taken(r)
+    return _rows8_call(lib().tvmattn_rowquant_fwd, x, tx, out)
+
+
+def tvmattn_gelu_jvp_fwd_q8(u, tu=None, out=None):
+    """Returns (q, s, tq, ts): the tanh-form GELU of u and its tangent gelu'(u) * tu as 8-bit rows."""
+    if out is None:
+        r = (_fast or _load_fast()).gelu_q8(u, tu)
+        if r is not None:
+            return _taken(r)
+    return _rows8_call(lib().tvmattn_gelu_jvp_fwd_q8, u, tu, out)
+
+
+def tvmattn_gate_adaln_jvp_fwd_q8(x, tx, h, th, c, tc, a, ta, b, tb, eps, out=None):
+    """z = x + RMSNorm^-(c) * h, then RMSNorm^-(z) * RMSNorm^-(a) + RMSNorm^-(b) as 8-bit rows, and the tangents of both.  Returns
+    (z, tz, q, s, tq, ts); `out`, if given, is that tuple (z may be x itself and tz tx itself).  h, th, c, tc None: no residual,
+    z and tz are x and tx.  All tangents None: none, tz, tq and ts are None."""
+    if out is None:
+        r = (_fast or _load_fast()).gate_adaln_q8(x, tx, h, th, c, tc, a, ta, b, tb, eps)
+        if r is not None:
+            r = _taken(r)
+            return r if h is not None else (x, tx) + r[2:]
+    tangent, gate = tx is not None, h is not None
+    tangents = (ta, tb) + ((th, tc) if gate else ())
+    if any((t is not None) != tangent for t in tangents) or (c is not None) != gate or (not gate and (th is not None or tc is not None)):
+        raise ValueError("a residual takes h and c, a tangent takes all of tx, ta, tb and, with a residual, th and tc")
+    mods = [m for m in (a, b, c, ta, tb, tc) if m is not None]
+    B, T, C, dt = _adaln_args(x, tx if tangent else x, mods)
+    _here(x)
+    for t in (tx, h, th):
+        if t is not None and (t.shape != x.shape or t.dtype != x.dtype or not t.is_contiguous() or t.device != x.device):
+            raise ValueError("the branch output and the tangents must look like x")
+    if out is None:
+        z, tz = (torch.empty_like(x) if gate else None), (torch.empty_like(x) if gate and tangent else None)
+        rows = _rows8_out(x.shape, x.device, tangent, None)
+    else:
+        z, tz, *rows = out
+        if not gate:   # z and tz are x and tx, or not given
+            if any(t is not None and t is not u for t, u in ((z, x), (tz, tx))):
+                raise ValueError("without a residual z is x and tz is tx")
+            z = tz = None
+        elif z is None or (tz is None) == tangent or any(
+                t is not None and (t.shape != x.shape or t.dtype != x.dtype or not t.is_contiguous() or t.device != x.device)
+                for t in (z, tz)):
+            raise ValueError("z and tz must look like x")
+        rows = _rows8_out(x.shape, x.device, tangent, rows)
+    q, s, tq, ts = rows
+    _check(lib().tvmattn_gate_adaln_jvp_fwd_q8(B, T, C, dt, x.data_ptr(), _ptr(tx), _ptr(h), _ptr(th), _ptr(c), _ptr(tc), a.data_ptr(),
+                                               _ptr(ta), b.data_ptr(), _ptr(tb), float(eps), _ptr(z), _ptr(tz), q.data_ptr(),
+                                               s.data_ptr(), _ptr(tq), _ptr(ts), _stream()))
+    return (z, tz, q, s, tq, ts) if gate else (x, tx, q, s, tq, ts)
+
+
+def tvmattn_linear_jvp_fwd_q8(xq, xs, txq, txs, wq, ws, bias=None, dtype=torch.bfloat16, out=None):
+    """Returns (y, ty): the linear layer of 8-bit rows xq ([..., K] int8, or 2-D [R, K] views with a row pitch) with scales xs [...]
+    and an 8-bit weight wq [F, K] with scales ws [F], in `dtype` (bfloat16 or float32, the bias's too).  txq, txs None: no tangent,
+    ty is None.  `out`: preallocated (y, ty), contiguous [..., F] or 2-D [R, F] views with a row pitch."""
+    if out is None:
+        r = (_fast or _load_fast()).linear_q8(xq, xs, txq, txs, wq, ws, bias, dtype is torch.bfloat16 if dtype in
+                                              (torch.bfloat16, torch.float32) else None)
+        if r is not None:
+            return _taken(r)
+    if wq.dim() != 2 or wq.dtype != torch.int8 or not wq.is_contiguous() or wq.device != xq.device:
+        raise ValueError("the weight must be a contiguous int8 [F, K] tensor on the rows' device")
+    F, K = wq.shape
+    if ws.shape != (F,) or ws.dtype != torch.float32 or not ws.is_contiguous() or ws.device != xq.device:
+        raise ValueError("the weight's scales must be a contiguous float32 [F] tensor on its device")
+    if xq.dtype != torch.int8 or xq.dim() < 1:
+        raise ValueError("rows must be int8 [..., K]")
+    R, ldx = _pitched(xq, K, "xq")
+    tangent = txq is not None
+    if tangent != (txs is not None):
+        raise ValueError("the tangent's rows and scales come together")
+    if tangent and (txq.shape != xq.shape or txq.dtype != xq.dtype or txq.stride() != xq.stride() or txq.device != xq.device):
+        raise ValueError("rows and their tangent must agree in shape, dtype and layout")
+    for t in (xs, txs):
+        if t is not None and (t.shape != xq.shape[:-1] or t.dtype != torch.float32 or not t.is_contiguous() or t.device != xq.device):
+            raise ValueError("scales must be contiguous float32 tensors, one value per row")
+    if dtype not in (torch.bfloat16, torch.float32):
+        raise ValueError(f"unsupported dtype {dtype}")
+    if bias is not None and (bias.shape != (F,) or bias.dtype != dtype or not bias.is_contiguous() or bias.device != xq.device):
+        raise ValueError("the bias must be a contiguous [F] tensor of the output's dtype on the rows' device")
+    if out is None:
+        shape = xq.shape[:-1] + (F,)
+        out = tuple(torch.empty(shape, dtype=dtype, device=xq.device) if n == 0 or tangent else None for n in range(2))
+    y, ty = out
+    Ry, ldy = _pitched(y, F, "y")
+    if Ry != R or y.dtype != dtype or (ty is None) == tangent or (tangent and (ty.shape != y.shape or ty.stride() != y.stride() or
+                                                                              ty.dtype != dtype or ty.device != y.device)):
+        raise ValueError("outputs must be [R, F] tensors of one dtype and layout, the second None without a tangent")
+    _check(lib().tvmattn_linear_jvp_fwd_q8(R, K, F, TVMATTN_BF16 if dtype == torch.bfloat16 else TVMATTN_F32, xq.data_ptr(),
+                                           xs.data_ptr(), _ptr(txq), _ptr(txs), ldx, wq.data_ptr(), ws.data_ptr(), _ptr(bias),
+                                           y.data_ptr(), _ptr(ty), ldy, _stream()))
+    return y, ty

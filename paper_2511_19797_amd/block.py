@@ -55,6 +55,35 @@ def block_jvp_fwd(x, tx, mods, tmods, params, H, eps, qk_eps):
     return z, tz, s
 
 
+WEIGHTS = ("wqkv", "wo", "w1", "w2")
+
+
+def block_q8_params(params):
+    """block_jvp_fwd's parameters for block_jvp_fwd_q8: the four weights as 8-bit rows, (int8 [F,K], scales [F]), worked out once;
+    everything else as it is."""
+    return {n: tvm.tvmattn_rowquant_fwd(t)[:2] if n in WEIGHTS else t for n, t in params.items()}
+
+
+def block_jvp_fwd_q8(x, tx, mods, tmods, q8_params, H, eps, qk_eps):
+    """block_jvp_fwd where no gradient will be taken (sampling, the target network of the loss), its linear layers in 8 bits: every
+    operand of theirs leaves the operator before it as 8-bit rows.  q8_params: from block_q8_params.  Returns (z, tz)."""
+    B, T, C = x.shape
+    d = C // H
+    p = q8_params
+    _, _, *u1 = tvm.tvmattn_gate_adaln_jvp_fwd_q8(x, tx, None, None, None, None, mods["a1"], tmods["a1"], mods["b1"], tmods["b1"], eps)
+    qkv, tqkv = tvm.tvmattn_linear_jvp_fwd_q8(*u1, *p["wqkv"], p["bqkv"])
+    q5, tq5 = qkv.view(B, T, 3, H, d), tqkv.view(B, T, 3, H, d)
+    (q, tq), (k, tk), (v, tv) = ((_heads(q5, i), _heads(tq5, i)) for i in range(3))
+    qn, tqn, kn, tkn = tvm.tvmattn_qknorm_jvp_fwd(q, tq, k, tk, p["gq"], p["gk"], qk_eps)
+    o, to, _, _ = tvm.tvmattn_jvp_fwd(qn, kn, v, tqn, tkn, tv, save=False)        # o laid out like qn
+    h1, th1 = tvm.tvmattn_linear_jvp_fwd_q8(*tvm.tvmattn_rowquant_fwd(_rows(o), _rows(to)), *p["wo"], p["bo"])
+    x1, tx1, *u2 = tvm.tvmattn_gate_adaln_jvp_fwd_q8(x, tx, h1.view(B, T, C), th1.view(B, T, C), mods["c1"], tmods["c1"], mods["a2"],
+                                                     tmods["a2"], mods["b2"], tmods["b2"], eps)
+    act = tvm.tvmattn_gelu_jvp_fwd_q8(*tvm.tvmattn_linear_jvp_fwd_q8(*u2, *p["w1"], p["b1"]))
+    h2, th2 = tvm.tvmattn_linear_jvp_fwd_q8(*act, *p["w2"], p["b2"])
+    return tvm.tvmattn_gate_jvp_fwd(x1, tx1, h2, th2, mods["c2"], tmods["c2"], eps, out=(x1, tx1))
+
+
 def block_jvp_bwd(x, tx, mods, tmods, params, H, eps, qk_eps, saved, gz, gtz):
     """The gradient of <gz, z> + <gtz, tz>.  Returns a dict: "x", "tx"; the modulation vectors "a1", "mb1", "c1", "a2",
     "mb2", "c2" and their tangents ("ta1", "tmb1", ...); the parameters by their names."""

@@ -430,9 +430,105 @@ PyObject* linear_bwd(PyObject*, PyObject* const* a, Py_ssize_t n) {
   });
 }
 
+// ---- 8-bit rows: int8 values and one float32 scale per row.
+Tensor scales_like(const Tensor& x, const Tensor& q) { return at::empty(q.sizes().slice(0, q.dim() - 1), x.options().dtype(at::kFloat)); }
+Tensor bytes_like(const Tensor& x) { return at::empty(x.sizes(), x.options().dtype(at::kChar)); }
+bool here(const Tensor& t) { return t.get_device() == c10::hip::current_device(); }
+
+PyObject* rows8(PyObject* const* a, Py_ssize_t n, bool gelu) {
+  return guarded([&]() -> PyObject* {
+    Args g{a, n};
+    const Tensor *x = g.t(0), *tx = g.opt(1);
+    int64_t R, ld;
+    int32_t dt;
+    if (!g.ok || !same_layout(*x, tx) || x->dim() < 1 || !small(x->size(-1)) || !rows(*x, x->size(-1), R, ld) || ld < x->size(-1) ||
+        !type_of(*x, dt) || !here(*x))
+      NOT_MINE;
+    Tensor o[4] = {bytes_like(*x)};
+    o[1] = scales_like(*x, *x);
+    if (tx != nullptr) o[2] = bytes_like(*x), o[3] = scales_like(*x, *x);
+    auto out = [&](int i) { return o[i].defined() ? ptr(o[i]) : nullptr; };
+    void* const st = stream();
+    const int C = (int)x->size(-1);
+    const int rc = gelu ? released(tvmattn_gelu_jvp_fwd_q8, (int)R, C, dt, ptr(x), ptr(tx), ld, out(0), (float*)out(1), out(2), (float*)out(3), st)
+                        : released(tvmattn_rowquant_fwd, (int)R, C, dt, ptr(x), ptr(tx), ld, out(0), (float*)out(1), out(2), (float*)out(3), st);
+    return result(rc, o);
+  });
+}
+// x tx
+PyObject* rowquant(PyObject*, PyObject* const* a, Py_ssize_t n) { return rows8(a, n, false); }
+// u tu
+PyObject* gelu_q8(PyObject*, PyObject* const* a, Py_ssize_t n) { return rows8(a, n, true); }
+
+// x tx h th c tc a ta b tb eps; without a residual the first two outputs are None
+PyObject* gate_adaln_q8(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded([&]() -> PyObject* {
+    Args g{a, n};
+    const Tensor *x = g.t(0), *tx = g.opt(1), *h = g.opt(2), *th = g.opt(3), *c = g.opt(4), *tc = g.opt(5), *s = g.t(6), *ts = g.opt(7),
+                 *b = g.t(8), *tb = g.opt(9);
+    const double eps = g.f(10);
+    const bool tan = tx != nullptr, gate = h != nullptr;
+    int32_t dt;
+    if (!g.ok || (c != nullptr) != gate || (ts != nullptr) != tan || (tb != nullptr) != tan || (th != nullptr) != (gate && tan) ||
+        (tc != nullptr) != (gate && tan))
+      NOT_MINE;
+    if (!token_args(*x, tan ? *tx : *x, {s, b}, dt) || (tan && !token_args(*x, *tx, {ts, tb}, dt)) ||
+        (gate && (!token_args(*x, *h, {c}, dt) || (tan && !token_args(*x, *th, {tc}, dt)))) || !here(*x))
+      NOT_MINE;
+    for (const Tensor* t : {tx, h, th})
+      if (t != nullptr && t->device() != x->device()) NOT_MINE;
+    Tensor o[6];
+    if (gate) o[0] = like(*x);
+    if (gate && tan) o[1] = like(*x);
+    o[2] = bytes_like(*x), o[3] = scales_like(*x, *x);
+    if (tan) o[4] = bytes_like(*x), o[5] = scales_like(*x, *x);
+    auto out = [&](int i) { return o[i].defined() ? ptr(o[i]) : nullptr; };
+    void* const st = stream();
+    const int rc = released(tvmattn_gate_adaln_jvp_fwd_q8, DIMS(x), dt, ptr(x), ptr(tx), ptr(h), ptr(th), (const float*)ptr(c),
+                            (const float*)ptr(tc), (const float*)ptr(s), (const float*)ptr(ts), (const float*)ptr(b),
+                            (const float*)ptr(tb), (float)eps, out(0), out(1), out(2), (float*)out(3), out(4), (float*)out(5), st);
+    return result(rc, o);
+  });
+}
+
+// xq xs txq txs wq ws bias, bfloat16 (or float32)
+PyObject* linear_q8(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded([&]() -> PyObject* {
+    Args g{a, n};
+    const Tensor *x = g.t(0), *xs = g.t(1), *tx = g.opt(2), *txs = g.opt(3), *w = g.t(4), *ws = g.t(5), *bias = g.opt(6);
+    const bool half = g.flag(7);
+    int64_t R, ldx;
+    if (!g.ok || (tx == nullptr) != (txs == nullptr)) NOT_MINE;
+    auto is_float = [](const Tensor& t) { return t.scalar_type() == at::kFloat && t.is_contiguous(); };
+    if (w->dim() != 2 || w->scalar_type() != at::kChar || x->scalar_type() != at::kChar || !w->is_contiguous() || !small(w->size(0)) ||
+        !small(w->size(1)) || w->size(0) == 0 || !rows(*x, w->size(1), R, ldx) || ldx < w->size(1) || !same_layout(*x, tx) || !here(*x))
+      NOT_MINE;
+    const auto each_row = x->sizes().slice(0, x->dim() - 1);
+    if (!is_float(*xs) || xs->sizes() != each_row || (txs != nullptr && (!is_float(*txs) || txs->sizes() != each_row)) || !is_float(*ws) ||
+        ws->dim() != 1 || ws->size(0) != w->size(0))
+      NOT_MINE;
+    const auto type = half ? at::kBFloat16 : at::kFloat;
+    if (bias != nullptr && (bias->dim() != 1 || bias->size(0) != w->size(0) || bias->scalar_type() != type || !bias->is_contiguous())) NOT_MINE;
+    for (const Tensor* t : {xs, txs, w, ws, bias})
+      if (t != nullptr && t->device() != x->device()) NOT_MINE;
+    const int64_t F = w->size(0);
+    auto shape = x->sizes().vec();
+    shape.back() = F;
+    const auto options = x->options().dtype(type);
+    Tensor o[2] = {at::empty(shape, options)};
+    if (tx != nullptr) o[1] = at::empty(shape, options);
+    void* const st = stream();
+    const int rc = released(tvmattn_linear_jvp_fwd_q8, (int)R, (int)w->size(1), (int)F, half ? TVMATTN_BF16 : TVMATTN_F32, ptr(x),
+                            (const float*)ptr(xs), ptr(tx), (const float*)ptr(txs), ldx, ptr(w), (const float*)ptr(ws), ptr(bias),
+                            ptr(o[0]), tx != nullptr ? ptr(o[1]) : nullptr, F, st);
+    return result(rc, o);
+  });
+}
+
 #define METHOD(name) {#name, (PyCFunction)(void (*)(void))name, METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {METHOD(jvp_fwd),  METHOD(jvp_bwd),  METHOD(qknorm_fwd), METHOD(bwd_qknorm), METHOD(adaln_fwd), METHOD(adaln_bwd),
                          METHOD(gate_fwd), METHOD(gate_bwd), METHOD(gelu_fwd),   METHOD(gelu_bwd),   METHOD(linear_fwd), METHOD(linear_bwd),
+                         METHOD(rowquant), METHOD(gelu_q8),  METHOD(gate_adaln_q8), METHOD(linear_q8),
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_fastcall", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 

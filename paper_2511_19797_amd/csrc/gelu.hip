@@ -8,7 +8,7 @@
 // Backward of <ga, a> + <gta, ta>:  gu = ga gelu' + gta tu gelu'',  gtu = gta gelu'.
 // Pointwise: 16 bytes per thread and tensor, float32 arithmetic, tanh(w) = 1 - 2 / (exp(2w) + 1) (exact limits for
 // large |w|: exp overflows to inf or underflows to 0).  About as much unpacked float32 arithmetic as memory time.
-#include "tvm_common.h"
+#include "gelu_math.h"
 
 namespace tvm {
 namespace {
@@ -18,7 +18,6 @@ namespace {
 #define GELU_MAXGRID 65535  // forward / backward at 16 x 1024 x 4608 against 114 / 177 us with 4 and 8192 workgroups)
 #endif
 constexpr int kNT = 256, kUnroll = GELU_UNROLL;
-constexpr float kK = 0.7978845608028654f, kC = 0.044715f, kTwoLog2e = 2.8853900817779268f;
 
 template <typename T>
 struct alignas(16) Chunk {
@@ -58,27 +57,6 @@ __device__ __forceinline__ void st_once(uint4* p, uint4 v) {
 #else
   *p = v;
 #endif
-}
-
-struct Gelu {
-  float half_1pt, g1, g2;  // (1 + t)/2, gelu', gelu''
-};
-// With e = exp(2w) and r = 1/(e + 1):  t = 1 - 2r,  (1 + t)/2 = 1 - r =: h,  1 - t^2 = 4 r h.  For large |w| the
-// exponential overflows to inf (r = 0, h = 1) or underflows to 0 (r = 1, h = 0): the limits come out exact.
-template <bool SECOND>
-__device__ __forceinline__ Gelu gelu_parts(float u) {
-  const float u2 = u * u;
-  const float e = __builtin_amdgcn_exp2f(u * fmaf(kTwoLog2e * kK * kC, u2, kTwoLog2e * kK));  // exp(2w)
-  const float r = __builtin_amdgcn_rcpf(e + 1.0f);
-  const float h = 1.0f - r;
-  const float q = u * r * h;                               // u (1 - t^2) / 4
-  const float wp = fmaf(3.0f * kK * kC, u2, kK);           // w'
-  Gelu g;
-  g.half_1pt = h;
-  g.g1 = fmaf(2.0f * q, wp, h);
-  // gelu'' = (1 - t^2) w' + u/2 (1 - t^2) (w'' - 2 t w'^2),  t = 1 - 2r
-  g.g2 = SECOND ? fmaf(2.0f * q, fmaf(wp * wp, fmaf(4.0f, r, -2.0f), 6.0f * kK * kC * u), 4.0f * r * h * wp) : 0.f;
-  return g;
 }
 
 // chunks: number of 16-byte chunks per tensor

@@ -5,6 +5,7 @@
 
 #include <mutex>
 
+#include "api_checks.h"
 #include "f32_mfma.h"
 #include "fwd_few.h"
 
@@ -13,8 +14,6 @@ namespace {
 inline void mark(void* const* events, int i, hipStream_t st) {
   if (events && events[i]) (void)hipEventRecord(static_cast<hipEvent_t>(events[i]), st);
 }
-
-inline bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 
 // One side's strides: all zero selects `dflt_*`; otherwise row pitch >= D and 16-byte multiples.  The whole tensor
 // must fit the 2^47-byte address space (which also keeps every later product of sizes and strides inside 64 bits).
@@ -71,27 +70,6 @@ int resolve(const tvmattn_desc* d, tvm::Shape* s) {
   return TVMATTN_OK;
 }
 
-// A buffer as the overlap check sees it: `dims` levels of (count, byte stride) around an innermost run of
-// `inner` bytes.  dims = 0 is a plain range.
-struct Buf {
-  const void* p;
-  int dims;
-  long long n[3], s[3];
-  long long inner;
-  long long extent() const {
-    long long e = inner;
-    for (int i = 0; i < dims; ++i) e += (n[i] - 1) * s[i];
-    return e;
-  }
-  bool same_layout(const Buf& o) const {
-    if (dims != o.dims || inner != o.inner) return false;
-    for (int i = 0; i < dims; ++i)
-      if (n[i] != o.n[i] || s[i] != o.s[i]) return false;
-    return true;
-  }
-};
-const void* const skip = reinterpret_cast<const void*>(uintptr_t(1));  // an entry the call's mode does not use
-inline Buf plain(const void* p, long long bytes) { return Buf{p, 0, {0, 0, 0}, {0, 0, 0}, bytes}; }
 // One side's [B,H,rows,D] tensor with that side's strides, levels sorted by descending stride.
 Buf side_buf(const void* p, const tvm::Shape& s, bool query_side, long long esz) {
   Buf b{p, 3, {s.B, s.H, query_side ? s.M : s.N},
@@ -108,61 +86,6 @@ Buf side_buf(const void* p, const tvm::Shape& s, bool query_side, long long esz)
       }
   return b;
 }
-// Do two buffers of ONE layout, `delta` bytes apart, share a byte?  They do iff delta = sum_k d_k s_k + e with
-// |d_k| < n_k and |e| < inner.  Where every stride is at least the extent of the levels inside it (any dense or
-// sliced tensor), what the inner levels can contribute is smaller than the stride, so only the two multiples of
-// s_k around delta can start a solution: a walk of depth `dims` with two branches per level.
-bool lattice_hit(const Buf& b, int level, long long delta) {
-  if (level == b.dims) return delta > -b.inner && delta < b.inner;
-  const long long st = b.s[level];
-  long long d0 = delta / st;
-  if (delta < 0 && d0 * st != delta) --d0;  // floor
-  for (long long d = d0; d <= d0 + 1; ++d)
-    if (d > -b.n[level] && d < b.n[level] && lattice_hit(b, level + 1, delta - d * st)) return true;
-  return false;
-}
-bool nested(const Buf& b) {
-  long long inside = b.inner;
-  for (int i = b.dims - 1; i >= 0; --i) {
-    if (b.s[i] < inside) return false;
-    inside = (b.n[i] - 1) * b.s[i] + inside;
-  }
-  return true;
-}
-bool overlap(const Buf& a, const Buf& b) {
-  const long long pa = (long long)reinterpret_cast<uintptr_t>(a.p), pb = (long long)reinterpret_cast<uintptr_t>(b.p);
-  if (pa + a.extent() <= pb || pb + b.extent() <= pa) return false;  // disjoint address ranges
-  if (a.same_layout(b) && nested(a)) return lattice_hit(a, 0, pb - pa);
-  return true;
-}
-// Every listed pointer must be non-null and 16-byte aligned, and no output may overlap an input or another
-// output.  Entries that the call's mode does not use are passed with p == skip (a null there is fine, and the
-// buffer takes no part in the overlap check).  `inout`: pairs (output index, input index) that may be the very
-// same buffer (an update in place).
-template <size_t NI, size_t NO>
-int check_bufs(const Buf (&in)[NI], const Buf (&out)[NO], int same_o = -1, int same_i = -1, int same_o2 = -1,
-               int same_i2 = -1) {
-  for (size_t i = 0; i < NI; ++i)
-    if (in[i].p != skip && (!in[i].p || !aligned16(in[i].p))) return TVMATTN_INVALID_ARG;
-  for (size_t o = 0; o < NO; ++o) {
-    if (out[o].p == skip) continue;
-    if (!out[o].p || !aligned16(out[o].p)) return TVMATTN_INVALID_ARG;
-    for (size_t i = 0; i < NI; ++i) {
-      if (in[i].p == skip) continue;
-      const bool allowed = ((int)o == same_o && (int)i == same_i) || ((int)o == same_o2 && (int)i == same_i2);
-      if (allowed && out[o].p == in[i].p) continue;
-      if (overlap(out[o], in[i])) return TVMATTN_INVALID_ARG;
-    }
-    for (size_t p = 0; p < o; ++p)
-      if (out[p].p != skip && overlap(out[o], out[p])) return TVMATTN_INVALID_ARG;
-  }
-  return TVMATTN_OK;
-}
-inline Buf unless(bool unused, Buf b) {
-  if (unused) b.p = skip;
-  return b;
-}
-inline long long esz_of(int dtype) { return dtype == TVMATTN_F32 ? 4 : 2; }
 // The dtype as the launchers of everything but the bf16 matrix-core kernels take it
 inline int generic_dtype(const tvmattn_desc* d) { return d->dtype | ((d->flags & TVMATTN_FLAG_PLAIN_ALU) != 0 ? tvm::kPlainAlu : 0); }
 inline bool plain_alu(const tvmattn_desc* d) { return (d->flags & TVMATTN_FLAG_PLAIN_ALU) != 0; }
@@ -171,7 +94,7 @@ inline bool plain_alu(const tvmattn_desc* d) { return (d->flags & TVMATTN_FLAG_P
 
 extern "C" {
 
-int tvmattn_version(void) { return 610; }  // 0.6.1: tvmattn_jvp_fwd_qknorm; 0.6.0: per-call flags instead of process-wide switches, tvmattn_jvp_bwd_timed, tvmattn_jvp_bwd_static, linear layers; 0.5.0: AdaLN modulation, residual gate, MLP activation; 0.4.0: QK-norm entry points; 0.3.0: M != N (the descriptor grew); 0.2.0: one-sided backward, forward that saves nothing
+int tvmattn_version(void) { return 700; }  // 0.7.0: 8-bit rows and linear layers; 0.6.1: tvmattn_jvp_fwd_qknorm; 0.6.0: per-call flags instead of process-wide switches, tvmattn_jvp_bwd_timed, tvmattn_jvp_bwd_static, linear layers; 0.5.0: AdaLN modulation, residual gate, MLP activation; 0.4.0: QK-norm entry points; 0.3.0: M != N (the descriptor grew); 0.2.0: one-sided backward, forward that saves nothing
 
 const char* tvmattn_strerror(int status) {
   switch (status) {
