@@ -122,6 +122,25 @@ __device__ __forceinline__ u32x4 descriptor(unsigned long long base, unsigned by
   return u32x4{(unsigned)base, (unsigned)(base >> 32), bytes, 0x00027000u};
 }
 
+// Slots of a contraction step: slot m is the gap behind its product m.  The NF fragment reads are spread over the slots from
+// f0 on; the others are free for loads (once these run out, the n-th load takes one that is not).
+template <int NP>
+struct FreeSlots {
+  int at[NP];
+};
+template <int NP, int NF>
+constexpr FreeSlots<NP> free_slots(int f0) {
+  FreeSlots<NP> s{};
+  int n = 0;
+  for (int m = f0; m < NP; ++m) {
+    bool read = false;
+    for (int f = 0; f < NF; ++f) read = read || m == f0 + f * (NP - f0) / NF;
+    if (!read) s.at[n++] = m;
+  }
+  for (int m = f0 + 1; n < NP; m = m + 2 < NP ? m + 2 : f0) s.at[n++] = m;
+  return s;
+}
+
 // The 256-row tile shapes (linear_pipe.hip); shape: k256 or k192.
 hipError_t launch_gemm_fwd(int shape, const GemmArgs& g, hipStream_t st);
 hipError_t launch_gemm_gx(int shape, const GemmArgs& g, hipStream_t st);

@@ -60,25 +60,6 @@ __device__ __forceinline__ void acc_to_bf16(unsigned& r0, unsigned& r1, unsigned
       : "a"(a0), "a"(a1), "a"(a2), "a"(a3), "a"(a4), "a"(a5), "a"(a6), "a"(a7));
 }
 
-// Slots of a contraction step: slot m is the gap behind its product m.  The NF fragment reads are spread over the slots from
-// f0 on; the others are free for loads (once these run out, the n-th load takes one that is not).
-template <int NP>
-struct FreeSlots {
-  int at[NP];
-};
-template <int NP, int NF>
-constexpr FreeSlots<NP> free_slots(int f0) {
-  FreeSlots<NP> s{};
-  int n = 0;
-  for (int m = f0; m < NP; ++m) {
-    bool read = false;
-    for (int f = 0; f < NF; ++f) read = read || m == f0 + f * (NP - f0) / NF;
-    if (!read) s.at[n++] = m;
-  }
-  for (int m = f0 + 1; n < NP; m = m + 2 < NP ? m + 2 : f0) s.at[n++] = m;
-  return s;
-}
-
 template <bool PTR, bool QTR, bool PARTIAL, int WJ>
 __global__ __launch_bounds__(256, 1) void gemm_pipe_kernel(GemmArgs g) {
   constexpr int kTI = 256, kTJ = 64 * WJ;

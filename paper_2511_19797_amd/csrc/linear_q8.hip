@@ -5,15 +5,10 @@
 // A 16-byte fragment holds 16 entries of a row where bf16 has 8, and one 32 x 32 x 32 product takes the cycles of a 32 x 32 x 16 one in
 // bf16: tiles of 128 bytes x N rows lie in LDS as they do there (Operand, linear_gemm.h, with two entries to its one), and a
 // contraction tile is 128 entries.  Computed transposed, D = W-fragment x X-fragment: a lane owns one token and 16 channels of a block.
-#include "linear_gemm.h"
-#include "q8.h"
+#include "linear_q8.h"
 
 namespace tvm {
 namespace {
-
-typedef __attribute__((ext_vector_type(4))) int i32x4;
-typedef __attribute__((ext_vector_type(16))) int i32x16;
-typedef __attribute__((ext_vector_type(4))) float f32x4;
 
 __device__ __forceinline__ i32x16 mfma_q8(bf16x8 a, bf16x8 b, i32x16 c) {
   return __builtin_amdgcn_mfma_i32_32x32x32_i8(__builtin_bit_cast(i32x4, a), __builtin_bit_cast(i32x4, b), c, 0, 0, 0);
@@ -21,14 +16,6 @@ __device__ __forceinline__ i32x16 mfma_q8(bf16x8 a, bf16x8 b, i32x16 c) {
 // All waves of the workgroup.  (Not __syncthreads, which waits for every load in flight.)
 __device__ __forceinline__ void barrier() { asm volatile("s_barrier" ::: "memory"); }
 
-constexpr int kBKQ = 128;  // contraction entries (bytes) per LDS tile
-
-// 16 bytes' worth of consecutive floats or bf16 values (four) as floats
-__device__ __forceinline__ f32x4 four(const float* p) { return *reinterpret_cast<const f32x4*>(p); }
-__device__ __forceinline__ f32x4 four(const bf16* p) {
-  const bf16x4 v = *reinterpret_cast<const bf16x4*>(p);
-  return f32x4{(float)v[0], (float)v[1], (float)v[2], (float)v[3]};
-}
 
 template <typename T, int N, int NST, int OCC>
 __global__ __launch_bounds__(256, OCC) void linear_q8_kernel(LinearQ8Args g) {
@@ -54,9 +41,7 @@ __global__ __launch_bounds__(256, OCC) void linear_q8_kernel(LinearQ8Args g) {
   OP ox, ow;
   ox.setup(lds0, wi, wave, lane, pitchX);
   ow.setup(lds0 + HALF, wj, wave, lane, pitchW);
-  // this lane's 16 bytes of a row, the same for all its loads: in the last tile they may lie past the row's end
-  const int pos = wave * 64 + lane, chunk = (pos & 7) ^ ((pos >> 4) & 7);
-  const unsigned cut = chunk * 16 >= last ? kNowhere : 0u;
+  const unsigned cut = lane_chunk(wave, lane) * 16 >= last ? kNowhere : 0u;  // of a row's last tile
   auto issue = [&](int t) {
     const bool end = t >= nct;  // beyond the end: loads that fetch nothing, so that the count of loads in flight stays the same
     const long long c0 = (long long)t * kBKQ;
@@ -132,20 +117,22 @@ __global__ __launch_bounds__(256, OCC) void linear_q8_kernel(LinearQ8Args g) {
 }
 
 template <typename T>
-hipError_t launch(const LinearQ8Args& a, hipStream_t st) {
+hipError_t launch_tiles(int shape, const LinearQ8Args& a, hipStream_t st) {
   const int sets = a.x[1] != nullptr ? 2 : 1;
-  const long long big = (long long)sets * ((a.R + 127) / 128) * ((a.F + 127) / 128);
-  if (big >= 256)
-    hipLaunchKernelGGL((linear_q8_kernel<T, 128, 4, 1>), dim3((unsigned)(((a.R + 127) / 128) * ((a.F + 127) / 128)), sets), dim3(256), 0, st, a);
-  else
-    hipLaunchKernelGGL((linear_q8_kernel<T, 64, 4, 2>), dim3((unsigned)(((a.R + 63) / 64) * ((a.F + 63) / 64)), sets), dim3(256), 0, st, a);
+  const dim3 grid((unsigned)tiles_of(shape, a.R, a.F), sets), block(256);
+  if (shape == k128) hipLaunchKernelGGL((linear_q8_kernel<T, 128, 4, 1>), grid, block, 0, st, a);
+  else hipLaunchKernelGGL((linear_q8_kernel<T, 64, 4, 2>), grid, block, 0, st, a);
   return hipGetLastError();
 }
 
 }  // namespace
 
 hipError_t launch_linear_q8(const LinearQ8Args& a, int dtype, hipStream_t st) {
-  return dtype == 1 ? launch<bf16>(a, st) : launch<float>(a, st);
+  const int sets = a.x[1] != nullptr ? 2 : 1;
+  if ((long long)sets * a.R <= kFewRows) return launch_linear_q8_few(a, dtype, st);
+  const int shape = pick_shape_q8(sets, a.R, a.F, a.K);
+  if (shape == k192) return launch_linear_q8_pipe(a, dtype, st);
+  return dtype == 1 ? launch_tiles<bf16>(shape, a, st) : launch_tiles<float>(shape, a, st);
 }
 
 }  // namespace tvm
