@@ -130,7 +130,7 @@ __global__ __launch_bounds__(NW == 1 ? 256 : 64 * NW) void rows_q8_kernel(RowsQ8
 // into LDS (with the tangents 24 bytes per column), and its four waves then take a row each, with no further barrier.
 constexpr int kNormWaves = 4;
 template <typename T, bool TAN, bool GATE, int NCH>
-__global__ __launch_bounds__(64 * kNormWaves) void gate_adaln_q8_kernel(GateAdalnQ8Args g) {
+__global__ __launch_bounds__(64 * kNormWaves, NCH <= 3 ? 4 : NCH == 4 ? 3 : 1) void gate_adaln_q8_kernel(GateAdalnQ8Args g) {
   constexpr int VEC = Chunk<T>::VEC, NV = GATE ? 3 : 2, PL = VEC / 4;
   extern __shared__ __attribute__((aligned(16))) float4 coef[];  // [vector, tangent of it ...][PL][chunks]: 16 bytes of a chunk per plane
   __shared__ float red[kNormWaves][2 * NV];
@@ -153,26 +153,35 @@ __global__ __launch_bounds__(64 * kNormWaves) void gate_adaln_q8_kernel(GateAdal
     }
   };
   int t = blockIdx.x * kNormWaves + wave;
-  if (t < g.T) load(t);
-
-  // where quad n (four columns) of a vector is kept
+  // Where quad n (four columns) of a vector is kept; this thread's quads are tid + 256 i.  All loads first, the first row's behind
+  // them: the prologue is one memory latency and two barriers.
+  constexpr int NQ = (NCH * PL + 3) / 4, NT = 64 * kNormWaves;
   auto place = [&](int vec, int n) { return (vec * PL + (PL == 1 ? 0 : n & 1)) * chunks + (PL == 1 ? n : n >> 1); };
   const float* const vs[3] = {g.a, g.b, g.c};
   const float* const tvs[3] = {g.ta, g.tb, g.tc};
+  float4 v4[NV][NQ], t4[TAN ? NV : 1][NQ];
+#pragma unroll
+  for (int k = 0; k < NV; ++k)
+#pragma unroll
+    for (int i = 0; i < NQ; ++i) {
+      const long long at = (long long)b * g.C + 4 * min(tid + NT * i, quads - 1);
+      v4[k][i] = *reinterpret_cast<const float4*>(vs[k] + at);
+      if constexpr (TAN) t4[k][i] = *reinterpret_cast<const float4*>(tvs[k] + at);
+    }
+  if (t < g.T) load(t);
+  __builtin_amdgcn_sched_barrier(0);
   float sums[2 * NV];
 #pragma unroll
   for (int k = 0; k < NV; ++k) {
-    const float4* const v4 = reinterpret_cast<const float4*>(vs[k] + (long long)b * g.C);
-    const float4* const t4 = TAN ? reinterpret_cast<const float4*>(tvs[k] + (long long)b * g.C) : nullptr;
     float s = 0.f, st = 0.f;
-    for (int n = tid; n < quads; n += 64 * kNormWaves) {
-      const float4 v = v4[n];
-      s = fmaf(v.x, v.x, fmaf(v.y, v.y, fmaf(v.z, v.z, fmaf(v.w, v.w, s))));
-      coef[place(TAN ? 2 * k : k, n)] = v;
+#pragma unroll
+    for (int i = 0; i < NQ; ++i) {
+      const float4 v = v4[k][i];
+      const float on = tid + NT * i < quads ? 1.f : 0.f;  // (quads past the last one: the last one again, weighing nothing)
+      s = fmaf(on, fmaf(v.x, v.x, fmaf(v.y, v.y, fmaf(v.z, v.z, v.w * v.w))), s);
       if constexpr (TAN) {
-        const float4 u = t4[n];
-        st = fmaf(v.x, u.x, fmaf(v.y, u.y, fmaf(v.z, u.z, fmaf(v.w, u.w, st))));
-        coef[place(2 * k + 1, n)] = u;
+        const float4 u = t4[k][i];
+        st = fmaf(on, fmaf(v.x, u.x, fmaf(v.y, u.y, fmaf(v.z, u.z, v.w * u.w))), st);
       }
     }
     sums[2 * k] = wave_sum_dpp(s);
@@ -192,14 +201,15 @@ __global__ __launch_bounds__(64 * kNormWaves) void gate_adaln_q8_kernel(GateAdal
       st += red[w][2 * k + 1];
     }
     const float r = 1.0f / sqrtf(s * invc + g.eps), r3m = r * r * r * (st * invc);
-    for (int n = tid; n < quads; n += 64 * kNormWaves) {  // (the entries that this thread wrote)
-      const int at = place(TAN ? 2 * k : k, n);
-      const float4 v = coef[at];
-      coef[at] = make_float4(v.x * r, v.y * r, v.z * r, v.w * r);
+#pragma unroll
+    for (int i = 0; i < NQ; ++i) {
+      const int n = tid + NT * i;
+      if (n >= quads) break;
+      const float4 v = v4[k][i];
+      coef[place(TAN ? 2 * k : k, n)] = make_float4(v.x * r, v.y * r, v.z * r, v.w * r);
       if constexpr (TAN) {
-        const int at2 = place(2 * k + 1, n);
-        const float4 u = coef[at2];
-        coef[at2] = make_float4(u.x * r - v.x * r3m, u.y * r - v.y * r3m, u.z * r - v.z * r3m, u.w * r - v.w * r3m);
+        const float4 u = t4[k][i];
+        coef[place(2 * k + 1, n)] = make_float4(u.x * r - v.x * r3m, u.y * r - v.y * r3m, u.z * r - v.z * r3m, u.w * r - v.w * r3m);
       }
     }
   }
@@ -250,9 +260,8 @@ __global__ __launch_bounds__(64 * kNormWaves) void gate_adaln_q8_kernel(GateAdal
           if constexpr (TAN) sxt = fmaf(v[j][e], w[j][e], sxt);
         }
       }
+      __builtin_amdgcn_sched_barrier(0);  // one chunk at a time: interleaved chunks cost more registers than they gain
     }
-    t += gridDim.x * kNormWaves;
-    if (t < g.T) load(t);  // the next row is on its way while this one is worked on
     const float r = 1.0f / sqrtf(wave_sum_dpp(sxx) * invc + g.eps);
     const float r3m = TAN ? r * r * r * (wave_sum_dpp(sxt) * invc) : 0.f;
     unsigned m = 0, tm = 0;
@@ -277,6 +286,7 @@ __global__ __launch_bounds__(64 * kNormWaves) void gate_adaln_q8_kernel(GateAdal
 #pragma unroll
       for (int e = 0; e < VEC; ++e) v[j][e] = fmaf(v[j][e] * r, ah[e], bh[e]);
       m = live ? mag_of<VEC>(v[j], m) : m;
+      __builtin_amdgcn_sched_barrier(0);
     }
     const Scale sc = scale_of(wave_max_dpp(m)), tsc = TAN ? scale_of(wave_max_dpp(tm)) : Scale{};
     if (lane == 0) {
@@ -291,6 +301,8 @@ __global__ __launch_bounds__(64 * kNormWaves) void gate_adaln_q8_kernel(GateAdal
         if constexpr (TAN) store_q8<VEC>(g.tq + at0 + c * VEC, w[j], tsc);
       }
     }
+    t += gridDim.x * kNormWaves;
+    if (t < g.T) load(t);
   }
 }
 
