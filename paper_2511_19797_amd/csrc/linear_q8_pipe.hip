@@ -5,7 +5,9 @@
 // fragments of two contraction steps ahead are read between the products, the loads of later tiles in the slots between.
 // Results: a lane owns a token and 16 channels of a block.  The token's scale is a register per block row.  A channel's scale and
 // bias belong to a register index, so every row of 16 lanes holds the 16 of its half, one per lane, and the arithmetic takes them
-// as row broadcasts (a data-parallel-primitive operand): two registers per block instead of 32.
+// as row broadcasts (a data-parallel-primitive operand): two registers per block instead of 32.  They come by asynchronous loads
+// into LDS, asked for when the output tile begins: with loads into registers the compiler waited, at the tile's end, for every
+// load in flight.
 #include <type_traits>
 
 #include "linear_gemm.h"
@@ -16,6 +18,7 @@ namespace {
 
 constexpr int kWI = 4;              // 32-row blocks of a wave
 constexpr unsigned kXTile = 32768;  // LDS: three X tiles, then two W tiles
+constexpr unsigned kScales = 3072;
 
 __device__ __forceinline__ void mfma_acc_q8(i32x16& acc, bf16x8 a, bf16x8 b) {
   asm volatile("v_mfma_i32_32x32x32_i8 %0, %1, %2, %0" : "+a"(acc) : "v"(a), "v"(b));
@@ -74,6 +77,11 @@ __device__ __forceinline__ void results(float (&v)[8], const i32x16& t, float xs
         "v"(xs), "v"(ws), "v"(bias), "n"(8 * H + 0), "n"(8 * H + 1), "n"(8 * H + 2), "n"(8 * H + 3), "n"(8 * H + 4), "n"(8 * H + 5), "n"(8 * H + 6), "n"(8 * H + 7));
 }
 
+// load_lds (linear_gemm.h) with 4 bytes per lane
+__device__ __forceinline__ void load_lds4(u32x4 srd, unsigned voff, unsigned lds) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dword %1, %2, 0 offen lds" ::"s"(lds), "v"(voff), "s"(srd) : "memory", "m0");
+}
+
 template <typename T>
 __global__ __launch_bounds__(256, 1) void q8_pipe_kernel(LinearQ8Args g, TileOrder order) {
   constexpr int kTI = 256, WJ = 3, kTJ = 64 * WJ;
@@ -85,9 +93,11 @@ __global__ __launch_bounds__(256, 1) void q8_pipe_kernel(LinearQ8Args g, TileOrd
   constexpr int NF = kWI + WJ;                 // fragments per contraction step
   constexpr int LX = OX::LOADS, LW = OW::LOADS;
   constexpr int STORES = (WIDE ? 4 : 2) * NP;  // stores of a wave per output tile
-  constexpr int SCALES = kWI + 2 * WJ;         // loads of scales and biases of a wave per output tile
-  constexpr int YOUNGER = LX + STORES + SCALES < 63 ? LX + STORES + SCALES : 63;
-  __shared__ __attribute__((aligned(1024))) char lds[3 * kXTile + 2 * kWTile];
+  constexpr int SCALES = 3;                    // loads of scales and biases of a wave per output tile
+  constexpr int YOUNGER = LX + STORES + SCALES;
+  static_assert(YOUNGER < 64, "vmcnt is six bits");
+  // (behind the tiles, twice: the scales of an output tile's 256 rows and 192 columns and the columns' biases, 1 KB each)
+  __shared__ __attribute__((aligned(1024))) char lds[3 * kXTile + 2 * kWTile + 2 * kScales];
   const int lane = threadIdx.x & 63, ic = lane & 31, hh = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int wi = wave & 1, wj = wave >> 1;
@@ -165,26 +175,16 @@ __global__ __launch_bounds__(256, 1) void q8_pipe_kernel(LinearQ8Args g, TileOrd
     else xf[kk][f - WJ] = ox.frag(f - WJ, kk);
   };
 
-  // Scales of the output tile's rows and columns, and biases (set 0 only); beyond the edges zeros.  A column's belongs to
-  // register 8 q4 + e of its half's lanes: lane 4 q4 + e of each row of 16.
-  float xs[kWI], ws[WJ], bias[WJ];
-  const int column = 8 * ((lane & 15) >> 2) + 4 * hh + (lane & 3);
-  auto scales_load = [&](const Where& w) {
-    const __amdgpu_buffer_rsrc_t rx = __builtin_amdgcn_make_buffer_rsrc(const_cast<float*>(w.set == 0 ? g.xs[0] : g.xs[1]) + w.i0, 0,
-                                                                        min(g.R - w.i0, kTI) * 4, 0x00027000);
-    const __amdgpu_buffer_rsrc_t rw = __builtin_amdgcn_make_buffer_rsrc(const_cast<float*>(g.ws), 0, g.F * 4, 0x00027000);
-    const __amdgpu_buffer_rsrc_t rb = __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(g.bias), 0,
-                                                                        g.bias != nullptr && w.set == 0 ? g.F * (int)sizeof(T) : 0, 0x00027000);
-#pragma unroll
-    for (int a = 0; a < kWI; ++a)
-      xs[a] = __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(rx, ((wi * kWI + a) * 32 + ic) * 4, 0, 0));
-#pragma unroll
-    for (int b = 0; b < WJ; ++b) {
-      const int f = w.j0 + (wj * WJ + b) * 32 + column;
-      ws[b] = __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(rw, f * 4, 0, 0));
-      if constexpr (WIDE) bias[b] = __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(rb, f * 4, 0, 0));
-      else bias[b] = __builtin_bit_cast(float, (unsigned)(unsigned short)__builtin_amdgcn_raw_buffer_load_b16(rb, f * 2, 0, 0) << 16);
-    }
+  // Scales of the output tile's rows and columns, and biases (set 0 only), into half `par` of their place; beyond the edges zeros.
+  // Every wave fetches 64 values' worth of each.
+  const unsigned ldss = ldsw + 2 * kWTile;
+  auto scales_load = [&](const Where& w, unsigned par) {
+    const unsigned at = ldss + par * kScales + (unsigned)wave * 256u, v = (unsigned)(wave * 64 + lane) * 4u;
+    const int cols = min(g.F - w.j0, kTJ);
+    load_lds4(descriptor((unsigned long long)(uintptr_t)((w.set == 0 ? g.xs[0] : g.xs[1]) + w.i0), (unsigned)min(g.R - w.i0, kTI) * 4u), v, at);
+    load_lds4(descriptor((unsigned long long)(uintptr_t)(g.ws + w.j0), (unsigned)cols * 4u), v, at + 1024u);
+    load_lds4(descriptor((unsigned long long)(uintptr_t)(static_cast<const T*>(g.bias) + w.j0),
+                         g.bias != nullptr && w.set == 0 ? (unsigned)(cols * (int)sizeof(T)) : 0u), v, at + 2048u);
   };
   auto start = [&](int a) {  // accumulators of block row a from 0, by a product of zeros
     const bf16x8 zero = __builtin_bit_cast(bf16x8, u32x4{0u, 0u, 0u, 0u});
@@ -198,7 +198,7 @@ __global__ __launch_bounds__(256, 1) void q8_pipe_kernel(LinearQ8Args g, TileOrd
   // 4 KB.  A chunk holds 8 rows (16 of 64 bytes); 16-byte chunks within them are swizzled, and in rows 16 to 31 the 8-byte
   // halves that the two half-waves write change places, so that no two lanes meet in a bank.
   typedef __attribute__((ext_vector_type(2))) unsigned u32x2;
-  auto write_out = [&](const Where& w) {
+  auto write_out = [&](const Where& w, unsigned par) {
     typedef u32x2 __attribute__((address_space(3))) * wp2;
     typedef f32x4 __attribute__((address_space(3))) * wp4;
     typedef const u32x4 __attribute__((address_space(3))) * rp;
@@ -217,6 +217,19 @@ __global__ __launch_bounds__(256, 1) void q8_pipe_kernel(LinearQ8Args g, TileOrd
     // read side: lane -> row r8 of 8 (16), chunk
     const unsigned rd128 = slot_x + (unsigned)(lane >> 3) * 128u, rd64 = slot_x + (unsigned)(lane >> 2) * 64u;
     const unsigned out128 = (unsigned)(lane >> 3) * pitch + (unsigned)(lane & 7) * 16u, out64 = (unsigned)(lane >> 2) * pitch + (unsigned)(lane & 3) * 16u;
+    typedef const float __attribute__((address_space(3))) * fp;
+    typedef const unsigned short __attribute__((address_space(3))) * sp;
+    // A column's scale and bias belong to register 8 q4 + e of its half's lanes: lane 4 q4 + e of each row of 16.
+    const unsigned sc = ldss + par * kScales, column = (unsigned)(wj * (WJ * 32) + 8 * ((lane & 15) >> 2) + 4 * hh + (lane & 3));
+    float xs[kWI], ws[WJ], bias[WJ];
+#pragma unroll
+    for (int a = 0; a < kWI; ++a) xs[a] = *(fp)(uintptr_t)(sc + (unsigned)((wi * kWI + a) * 32 + ic) * 4u);
+#pragma unroll
+    for (int b = 0; b < WJ; ++b) {
+      ws[b] = *(fp)(uintptr_t)(sc + 1024u + (column + b * 32) * 4u);
+      if constexpr (WIDE) bias[b] = *(fp)(uintptr_t)(sc + 2048u + (column + b * 32) * 4u);
+      else bias[b] = __builtin_bit_cast(float, (unsigned)*(sp)(uintptr_t)(sc + 2048u + (column + b * 32) * 2u) << 16);
+    }
     u32x4 v[4];
     auto park = [&](int n) __attribute__((always_inline)) {     // piece n into its half of the place
       const int a = n / NS, b0 = n % NS * WB, nb = WJ - b0 < WB ? WJ - b0 : WB;
@@ -280,7 +293,8 @@ __global__ __launch_bounds__(256, 1) void q8_pipe_kernel(LinearQ8Args g, TileOrd
 
   // Start: tiles 0 and 1 on their way, the accumulators at 0, the first fragments.
   Where w = locate(wg);
-  scales_load(w);
+  unsigned par = 0;
+  scales_load(w, par);
   open(w);
 #pragma unroll
   for (int n = 0; n < 2; ++n) {
@@ -372,11 +386,16 @@ __global__ __launch_bounds__(256, 1) void q8_pipe_kernel(LinearQ8Args g, TileOrd
     }
     if (left == 0) {
       mfma_settle();
-      write_out(locate(wg));
+      if (nct == 1) {  // (no other barrier since the scales were asked for)
+        dma_wait();
+        asm volatile("s_barrier" ::: "memory");
+      }
+      write_out(locate(wg), par);
       fresh = 1;
       wg += wg_per_xcd;
       if (wg >= id_end) break;
-      scales_load(locate(wg));
+      par ^= 1;
+      scales_load(locate(wg), par);
       left = nct;
       passed = quiet = min(quiet, left);
       __builtin_amdgcn_s_waitcnt(0xc07f);
