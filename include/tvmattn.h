@@ -499,7 +499,7 @@ int tvmattn_gate_adaln_jvp_fwd_q8(int B, int T, int C, int dtype,
  *        bias      [F] dtype, or NULL
  *   out: y, ty     [R,F] dtype (float32 or bfloat16), rows ldy elements apart (0 = F: dense)
  * The sums are exact (32-bit integers); they are scaled in float32 and rounded once.  K and ldx must be multiples of 16, F and
- * ldy of 8, K at most 2^16, F and the pitches at most 2^20; otherwise TVMATTN_UNSUPPORTED.  One launch, no workspace.
+ * ldy of 8, K at most 2^16, F and the pitches at most 2^20, R at most 2^30, R F at most 2^38; otherwise TVMATTN_UNSUPPORTED.  One launch, no workspace.
  */
 int tvmattn_linear_jvp_fwd_q8(int R, int K, int F, int dtype, const void* xq, const float* xs, const void* txq,
                               const float* txs, long long ldx, const void* wq, const float* ws, const void* bias,

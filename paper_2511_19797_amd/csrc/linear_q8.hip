@@ -17,44 +17,93 @@ __device__ __forceinline__ i32x16 mfma_q8(bf16x8 a, bf16x8 b, i32x16 c) {
 __device__ __forceinline__ void barrier() { asm volatile("s_barrier" ::: "memory"); }
 
 
+// N x N output tiles, one to a workgroup of four waves, for shapes with few of the 256-row tiles.  As in gemm_small_kernel (linear.hip):
+// a wave reads the fragments of the next contraction tile between the products of this one, the loads run NST - 2 tiles ahead,
+// counted rather than drained, and their descriptors move by additions.  Scales and biases are asked for first of all.
 template <typename T, int N, int NST, int OCC>
-__global__ __launch_bounds__(256, OCC) void linear_q8_kernel(LinearQ8Args g) {
+__global__ __launch_bounds__(256, OCC) void linear_q8_kernel(LinearQ8Args g, TileOrder order) {
   constexpr int W = N / 64;  // blocks of 32 x 32 per wave, either way
   using OP = Operand<false, N>;
   constexpr unsigned HALF = N * 128u, BUF = 2 * HALF;  // a stage: X tile, W tile
-  constexpr int LOADS = OP::LOADS, BOTH = 2 * LOADS;
+  constexpr int LOADS = 2 * OP::LOADS;                 // wave-loads per wave and contraction tile
   constexpr unsigned OUT_REGION = 32 * (64 * W + 16);  // per wave, for store_tile_coalesced
-  static_assert((NST - 2) * BOTH < 64 && 4 * OUT_REGION <= NST * BUF && NST * BUF * OCC <= 160 * 1024, "stages");
+  static_assert(NST >= 4 && (NST - 2) * LOADS < 64 && 4 * OUT_REGION <= NST * BUF && NST * BUF * OCC <= 160 * 1024, "stages");
   __shared__ __attribute__((aligned(1024))) char lds[NST * BUF];
-  const int nI = (g.R + N - 1) / N, nJ = (g.F + N - 1) / N;
+  const int nI = (g.R + N - 1) / N, nJ = (g.F + N - 1) / N, total = order.sets * nI * nJ;
+  // XCD x owns the x-th eighth of the tiles, which run in groups of kGI tile rows, down the group first (linear_pipe.hip)
+  const int wg = (int)(blockIdx.x & 7) * ((total + 7) >> 3) + (int)(blockIdx.x >> 3);
+  if (wg >= min(total, ((int)(blockIdx.x & 7) + 1) * ((total + 7) >> 3))) return;
   const int lane = threadIdx.x & 63, ic = lane & 31, hh = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wi = wave & 1, wj = wave >> 1;
-  const int it = (int)(blockIdx.x % (unsigned)nI), jt = (int)(blockIdx.x / (unsigned)nI), set = blockIdx.y;
-  if (jt >= nJ) return;
-  const int i0 = it * N, j0 = jt * N, nct = (g.K + kBKQ - 1) / kBKQ, last = g.K - (nct - 1) * kBKQ;
-  const signed char* const x = set == 0 ? g.x[0] : g.x[1];
-  const float* const xs = set == 0 ? g.xs[0] : g.xs[1];
-  T* const y = static_cast<T*>(set == 0 ? g.y[0] : g.y[1]);
+  const Quotient z = divide((unsigned)wg, order.by_set), grp = divide(z.r, order.by_group);
+  const int it_first = (int)grp.q * kGI;
+  const Quotient tile = nI - it_first >= kGI ? Quotient{grp.r / kGI, grp.r % kGI} : divide(grp.r, order.by_rest);
+  const bool second = z.q != 0;
+  const int i0 = (it_first + (int)tile.r) * N, j0 = (int)tile.q * N, jw = j0 + wj * (W * 32);
+  const int nct = (g.K + kBKQ - 1) / kBKQ, last = g.K - (nct - 1) * kBKQ;  // contraction tiles, bytes of a row in the last one
+  const signed char* const x = second ? g.x[1] : g.x[0];
   const unsigned pitchX = (unsigned)g.ldx, pitchW = (unsigned)g.K;
-  const int validX = min(g.R - i0, N), validW = min(g.F - j0, N);
   const unsigned lds0 = lds_addr_of(lds);
   OP ox, ow;
   ox.setup(lds0, wi, wave, lane, pitchX);
   ow.setup(lds0 + HALF, wj, wave, lane, pitchW);
+
+  float xs[W];
+  f32x4 ws[W][4], bias[W][4];
+  {
+    const float* const from = second ? g.xs[1] : g.xs[0];
+    const bool biased = g.bias != nullptr && !second;
+#pragma unroll
+    for (int a = 0; a < W; ++a) xs[a] = from[min(i0 + (wi * W + a) * 32 + ic, g.R - 1)];
+#pragma unroll
+    for (int b = 0; b < W; ++b)
+#pragma unroll
+      for (int q4 = 0; q4 < 4; ++q4) {
+        const int f = min(jw + b * 32 + 8 * q4 + 4 * hh, g.F - 4);  // (F is a multiple of 8: four channels are in range together)
+        ws[b][q4] = four(g.ws + f);
+        bias[b][q4] = biased ? four(static_cast<const T*>(g.bias) + f) : f32x4{0.f, 0.f, 0.f, 0.f};
+      }
+  }
+
+  // The loads' cursor: descriptors (first byte, size for the bounds check) and lane offsets of contraction tile c_t
+  u32x4 sx = descriptor((unsigned long long)(uintptr_t)(x + (long long)i0 * g.ldx), (unsigned)(min(g.R - i0, N) - 1) * pitchX + (unsigned)g.K);
+  u32x4 sw = descriptor((unsigned long long)(uintptr_t)(g.w + (long long)j0 * g.K), (unsigned)(min(g.F - j0, N) - 1) * pitchW + (unsigned)g.K);
   const unsigned cut = lane_chunk(wave, lane) * 16 >= last ? kNowhere : 0u;  // of a row's last tile
-  auto issue = [&](int t) {
-    const bool end = t >= nct;  // beyond the end: loads that fetch nothing, so that the count of loads in flight stays the same
-    const long long c0 = (long long)t * kBKQ;
-    const u32x4 sx = descriptor((unsigned long long)(uintptr_t)(x + (long long)i0 * g.ldx + c0),
-                                end ? 0u : (unsigned)(validX - 1) * pitchX + (unsigned)(g.K - (int)c0));
-    const u32x4 sw = descriptor((unsigned long long)(uintptr_t)(g.w + (long long)j0 * g.K + c0),
-                                end ? 0u : (unsigned)(validW - 1) * pitchW + (unsigned)(g.K - (int)c0));
-    const unsigned l = lds0 + (unsigned)(t % NST) * BUF + (unsigned)wave * 1024u, c = t == nct - 1 ? cut : 0u;
-#pragma unroll
-    for (int n = 0; n < LOADS; ++n) load_lds(sx, ox.voff[0] | c, (unsigned)(n * OP::ROWS_STEP) * pitchX, l, n * 4096);
-#pragma unroll
-    for (int n = 0; n < LOADS; ++n) load_lds(sw, ow.voff[0] | c, (unsigned)(n * OP::ROWS_STEP) * pitchW, l, (int)HALF + n * 4096);
+  unsigned vx = ox.voff[0], vw = ow.voff[0];
+  int c_t = 0;
+  auto settle = [&]() {
+    if (c_t == nct - 1) {
+      vx |= cut;
+      vw |= cut;
+    }
+    if (c_t >= nct) sx[2] = sw[2] = 0;  // beyond the end: loads that fetch nothing, so that the count of loads in flight stays the same
   };
+  auto move = [&]() {
+    ++c_t;
+    sx = descriptor(((unsigned long long)sx[1] << 32 | sx[0]) + 128ull, sx[2] - 128u);
+    sw = descriptor(((unsigned long long)sw[1] << 32 | sw[0]) + 128ull, sw[2] - 128u);
+    settle();
+  };
+  // wave-load n of the cursor's tile into the stage at `to`
+  auto issue = [&](unsigned to, int n) __attribute__((always_inline)) {
+    const unsigned l = lds0 + to + (unsigned)wave * 1024u;
+    if (n < OP::LOADS) load_lds(sx, vx, (unsigned)(n * OP::ROWS_STEP) * pitchX, l, n * 4096);
+    else load_lds(sw, vw, (unsigned)((n - OP::LOADS) * OP::ROWS_STEP) * pitchW, l, (int)HALF + (n - OP::LOADS) * 4096);
+  };
+  bf16x8 xf[2][4][W], wf[2][4][W];
+  auto fetch = [&](int set, int kk, unsigned at) {
+#pragma unroll
+    for (int a = 0; a < W; ++a) xf[set][kk][a] = ox.frag(a, kk, at);
+#pragma unroll
+    for (int b = 0; b < W; ++b) wf[set][kk][b] = ow.frag(b, kk, at);
+  };
+  settle();
+#pragma unroll
+  for (int n = 0; n < NST - 1; ++n) {
+#pragma unroll
+    for (int y = 0; y < LOADS; ++y) issue(n * BUF, y);
+    move();
+  }
   i32x16 acc[W][W];
 #pragma unroll
   for (int a = 0; a < W; ++a)
@@ -62,45 +111,47 @@ __global__ __launch_bounds__(256, OCC) void linear_q8_kernel(LinearQ8Args g) {
     for (int b = 0; b < W; ++b)
 #pragma unroll
       for (int r = 0; r < 16; ++r) acc[a][b][r] = 0;
-  for (int t = 0; t < NST - 1; ++t) issue(t);
-  for (int t = 0; t < nct; ++t) {
-    dma_wait_keep<(NST - 2) * BOTH>();
-    barrier();  // tile t is there for everyone, and everyone is done with tile t - 1: its stage is refilled now
-    issue(t + NST - 1);
-    const unsigned at = (unsigned)(t % NST) * BUF;
+  dma_wait_keep<(NST - 2) * LOADS>();
+  barrier();
+#pragma unroll
+  for (int kk = 0; kk < 4; ++kk) fetch(0, kk, 0);
+  unsigned at = 0;  // tile t's stage
+  auto turn = [&](int set) {
+    const unsigned next = at + BUF == NST * BUF ? 0 : at + BUF, before = at == 0 ? (NST - 1) * BUF : at - BUF;
+    dma_wait_keep<(NST - 3) * LOADS>();
+    barrier();  // tile t + 1 is there for everyone, and everyone has tile t - 1 in registers: its stage is refilled now
 #pragma unroll
     for (int kk = 0; kk < 4; ++kk) {
-      bf16x8 xf[W], wf[W];
+      fetch(set ^ 1, kk, next);
 #pragma unroll
-      for (int a = 0; a < W; ++a) xf[a] = ox.frag(a, kk, at);
-#pragma unroll
-      for (int b = 0; b < W; ++b) wf[b] = ow.frag(b, kk, at);
+      for (int n = kk * LOADS / 4; n < (kk + 1) * LOADS / 4; ++n) issue(before, n);
+      __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
       for (int a = 0; a < W; ++a)
 #pragma unroll
-        for (int b = 0; b < W; ++b) acc[a][b] = mfma_q8(wf[b], xf[a], acc[a][b]);
+        for (int b = 0; b < W; ++b) acc[a][b] = mfma_q8(wf[set][kk][b], xf[set][kk][a], acc[a][b]);
+      __builtin_amdgcn_sched_barrier(0);
     }
+    move();
+    at = next;
+  };
+  for (int t = 0; t < nct; t += 2) {
+    turn(0);
+    if (t + 1 < nct) turn(1);
   }
   dma_wait();  // the loads past the end land in stages that the results are about to go through
   __syncthreads();
-  const int jw = j0 + wj * (W * 32);
   if (jw >= g.F) return;
+  T* const y = static_cast<T*>(second ? g.y[1] : g.y[0]);
   const unsigned lw = lds0 + (unsigned)wave * OUT_REGION;
-  const bool biased = g.bias != nullptr && set == 0;
 #pragma unroll
   for (int a = 0; a < W; ++a) {
     const int i = i0 + (wi * W + a) * 32 + ic;
-    const float s = xs[min(i, g.R - 1)];
     f32x16 out[W];
 #pragma unroll
     for (int b = 0; b < W; ++b)
 #pragma unroll
-      for (int q4 = 0; q4 < 4; ++q4) {
-        const int f = min(jw + b * 32 + 8 * q4 + 4 * hh, g.F - 4);  // (F is a multiple of 8: four channels are in range together)
-        const f32x4 ws = four(g.ws + f), bias = biased ? four(static_cast<const T*>(g.bias) + f) : f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-        for (int e = 0; e < 4; ++e) out[b][4 * q4 + e] = fmaf((float)acc[a][b][4 * q4 + e] * s, ws[e], bias[e]);
-      }
+      for (int r = 0; r < 16; ++r) out[b][r] = fmaf((float)acc[a][b][r] * xs[a], ws[b][r >> 2][r & 3], bias[b][r >> 2][r & 3]);
     if constexpr (sizeof(T) == 2) {
       store_tile_coalesced<W>(lw, y + jw, g.ldy, i0 + (wi * W + a) * 32, g.R, g.F - jw, out, 1.f, lane);
     } else if (i < g.R) {
@@ -119,9 +170,10 @@ __global__ __launch_bounds__(256, OCC) void linear_q8_kernel(LinearQ8Args g) {
 template <typename T>
 hipError_t launch_tiles(int shape, const LinearQ8Args& a, hipStream_t st) {
   const int sets = a.x[1] != nullptr ? 2 : 1;
-  const dim3 grid((unsigned)tiles_of(shape, a.R, a.F), sets), block(256);
-  if (shape == k128) hipLaunchKernelGGL((linear_q8_kernel<T, 128, 4, 1>), grid, block, 0, st, a);
-  else hipLaunchKernelGGL((linear_q8_kernel<T, 64, 4, 2>), grid, block, 0, st, a);
+  const dim3 grid((unsigned)small_workgroups(sets * tiles_of(shape, a.R, a.F))), block(kSmallThreads);
+  const TileOrder order = tile_order(shape, sets, a.R, a.F);
+  if (shape == k128) hipLaunchKernelGGL((linear_q8_kernel<T, 128, 4, 1>), grid, block, 0, st, a, order);
+  else hipLaunchKernelGGL((linear_q8_kernel<T, 64, 5, 2>), grid, block, 0, st, a, order);
   return hipGetLastError();
 }
 

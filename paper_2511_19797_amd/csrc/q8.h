@@ -42,9 +42,10 @@ inline int vec_of(int dtype) { return dtype == 1 ? 8 : 4; }
 inline bool rows_q8_supported(int C, int dtype) { return C % vec_of(dtype) == 0 && C / vec_of(dtype) <= kMaxChunksQ8; }
 inline bool norm_q8_supported(int C, int dtype) { return C % vec_of(dtype) == 0 && C / vec_of(dtype) <= kMaxChunksNormQ8; }
 // A sum of K products of magnitude 2^14 at most stays inside 32 bits for K <= 2^16.  Pitches up to 2^20: a tile's byte offsets
-// (256 rows x pitch) stay inside 32 bits.
-inline bool linear_q8_supported(int K, int F, long long ldx, long long ldy) {
-  return K % 16 == 0 && K <= (1 << 16) && F % 8 == 0 && F <= (1 << 20) && ldx % 16 == 0 && ldx <= (1ll << 20) && ldy % 8 == 0 &&
+// (256 rows x pitch) stay inside 32 bits.  At most 2^30 rows and 2^38 results: rows and output tiles of any shape are
+// counted in 31 bits, past the last one too.
+inline bool linear_q8_supported(int R, int K, int F, long long ldx, long long ldy) {
+  return R <= (1 << 30) && (long long)R * F <= (1ll << 38) && K % 16 == 0 && K <= (1 << 16) && F % 8 == 0 && F <= (1 << 20) && ldx % 16 == 0 && ldx <= (1ll << 20) && ldy % 8 == 0 &&
          ldy <= (1ll << 20);
 }
 

@@ -91,7 +91,7 @@ int tvmattn_linear_jvp_fwd_q8(int R, int K, int F, int dtype, const void* xq, co
   if (ldx < K || ldy < F) return TVMATTN_INVALID_ARG;
   const bool none = txq == nullptr;
   if (none != (txs == nullptr) || none != (ty == nullptr)) return TVMATTN_INVALID_ARG;
-  if (!tvm::linear_q8_supported(K, F, ldx, ldy)) return TVMATTN_UNSUPPORTED;
+  if (!tvm::linear_q8_supported(R, K, F, ldx, ldy)) return TVMATTN_UNSUPPORTED;
   const long long e = esz_of(dtype);
   Buf wscales = scales(ws, F);
   wscales.align = 16;  // (read four at a time)

@@ -67,7 +67,7 @@ __global__ __launch_bounds__(NW == 1 ? 256 : 64 * NW) void rows_q8_kernel(RowsQ8
   constexpr int VEC = Chunk<T>::VEC, SETS = GELU && TAN ? 2 : 1, PER_WG = NW == 1 ? 4 : 1;
   __shared__ unsigned red[SETS][NW];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const long long row = (long long)blockIdx.x * PER_WG + (NW == 1 ? wave : 0);
+  const long long row = ((long long)blockIdx.z * gridDim.x + blockIdx.x) * PER_WG + (NW == 1 ? wave : 0);
   if (row >= a.R) return;  // (NW > 1: the whole workgroup or nobody)
   const bool second = !GELU && blockIdx.y == 1;
   const T* x = static_cast<const T*>(second ? a.tx : a.x) + row * a.ld;
@@ -309,7 +309,9 @@ __global__ __launch_bounds__(64 * kNormWaves, NCH <= 3 ? 4 : NCH == 4 ? 3 : 1) v
 template <typename T, bool GELU, bool TAN>
 hipError_t launch_rows(const RowsQ8Args& a, hipStream_t st) {
   const int chunks = a.C / Chunk<T>::VEC, NW = chunks <= 256 ? 1 : chunks <= 1024 ? 4 : 16, NCH = (chunks + 64 * NW - 1) / (64 * NW);
-  const dim3 grid((unsigned)(NW == 1 ? (a.R + 3ll) / 4 : a.R), !GELU && a.tx != nullptr ? 2 : 1), block(NW == 1 ? 256 : 64 * NW);
+  constexpr long long kMaxX = 1ll << 20;  // (a dimension of a launch is limited to 2^32 - 1 threads)
+  const long long wgs = NW == 1 ? (a.R + 3ll) / 4 : a.R;
+  const dim3 grid((unsigned)std::min(wgs, kMaxX), !GELU && a.tx != nullptr ? 2 : 1, (unsigned)((wgs + kMaxX - 1) / kMaxX)), block(NW == 1 ? 256 : 64 * NW);
 #define TVM_ROWS(N, W) \
   if (NCH == N && NW == W) hipLaunchKernelGGL((rows_q8_kernel<T, GELU, TAN, N, W>), grid, block, 0, st, a);
   TVM_ROWS(1, 1) TVM_ROWS(2, 1) TVM_ROWS(3, 1) TVM_ROWS(4, 1)
