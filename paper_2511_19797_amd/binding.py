@@ -639,6 +639,8 @@ def _here(t):
 
 
 def _pitched(t, cols, what):
+    if cols == 0:
+        raise ValueError(f"{what}: rows without columns")
     R, ld = _rows(t, cols, what)
     if ld < cols:
         raise ValueError(f"{what}: rows overlap")
@@ -709,8 +711,8 @@ def tvmattn_gate_adaln_jvp_fwd_q8(x, tx, h, th, c, tc, a, ta, b, tb, eps, out=No
             return r if h is not None else (x, tx) + r[2:]
     tangent, gate = tx is not None, h is not None
     tangents = (ta, tb) + ((th, tc) if gate else ())
-    if any((t is not None) != tangent for t in tangents) or (c is not None) != gate or (not gate and (th is not None or tc is not None)):
-        raise ValueError("a residual takes h and c, a tangent takes all of tx, ta, tb and, with a residual, th and tc")
+    if a is None or b is None or any((t is not None) != tangent for t in tangents) or (c is not None) != gate or (not gate and (th is not None or tc is not None)):
+        raise ValueError("the modulation takes a and b, a residual h and c, a tangent all of tx, ta, tb and, with a residual, th and tc")
     mods = [m for m in (a, b, c, ta, tb, tc) if m is not None]
     B, T, C, dt = _adaln_args(x, tx if tangent else x, mods)
     _here(x)

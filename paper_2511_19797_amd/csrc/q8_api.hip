@@ -22,10 +22,10 @@ int rows_args(int R, int C, int dtype, const void* x, const void* tx, long long 
   if (R < 1 || C < 1 || ldx < 0) return TVMATTN_INVALID_ARG;
   if (!dtype_ok(dtype)) return TVMATTN_UNSUPPORTED;
   if (ldx == 0) ldx = C;
-  if (ldx < C || ldx > (1ll << 40)) return TVMATTN_INVALID_ARG;
+  if (ldx < C) return TVMATTN_INVALID_ARG;
   const bool none = tx == nullptr;
   if (none != (tq == nullptr) || none != (ts == nullptr)) return TVMATTN_INVALID_ARG;
-  if (!tvm::rows_q8_supported(C, dtype) || ldx % tvm::vec_of(dtype) != 0 || (long long)R * ldx > (1ll << 45)) return TVMATTN_UNSUPPORTED;
+  if (!tvm::rows_q8_supported(C, dtype) || ldx % tvm::vec_of(dtype) != 0 || ldx > (1ll << 45) / R) return TVMATTN_UNSUPPORTED;
   const long long e = esz_of(dtype), n = (long long)R * C;
   const Buf in[] = {pitched(x, R, C, ldx, e), unless(none, pitched(tx, R, C, ldx, e))};
   const Buf out[] = {plain(q, n), scales(s, R), unless(none, plain(tq, n)), unless(none, scales(ts, R))};

@@ -214,6 +214,8 @@ LINEAR = [
     (1, 16, 8), (1, 1152, 6912), (2, 48, 40), (7, 4608, 1152), (16, 1152, 1160), (17, 1168, 72), (33, 32, 8),
     (64, 128, 64), (65, 144, 72), (250, 768, 2304), (256, 1152, 1152), (500, 400, 1000), (129, 112, 136),
     (300, 4624, 264), (1000, 1152, 3456), (1030, 2320, 520), (2100, 64, 2056), (4000, 1152, 1152), (70, 65536, 16),
+    (9000, 64, 1160), (9000, 112, 1160), (9000, 208, 1160),   # several output tiles per workgroup, of one and two contraction tiles
+    (9, 1152, 40), (8, 2064, 1160), (16, 4608, 200),           # a handful of rows, two sets of them and one; 4 waves and 8
 ]
 
 
@@ -341,3 +343,103 @@ def test_two_streams_at_once():
     torch.cuda.synchronize()
     for a, b in zip(got, ref):
         assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1])
+
+
+# ---- the binding: native and Python ways, what it refuses
+def binding_calls():
+    t = norm_inputs(2, 5, 64, "bf16", 1)
+    d = {n: v.cuda() for n, v in t.items()}
+    x = d["x"].view(10, 64)
+    e = {n: v.cuda() for n, v in linear_inputs(10, 64, 40, 2).items()}
+    b = e["bias"].bfloat16()
+    wide = torch.randn(10, 192, device="cuda")
+    return {
+        "rowquant": (tvm.tvmattn_rowquant_fwd, [(x, None), (x, x), (wide[:, 64:128], wide[:, :64]), (d["x"], None)]),
+        "gelu_q8": (tvm.tvmattn_gelu_jvp_fwd_q8, [(x, None), (x, x), (wide[:, 64:128], wide[:, :64])]),
+        "gate_adaln_q8": (tvm.tvmattn_gate_adaln_jvp_fwd_q8, [
+            [d[n] for n in ORDER] + [EPS], [d["x"], d["tx"]] + [None] * 4 + [d[n] for n in ORDER[6:]] + [EPS],
+            [d["x"], None, d["h"], None, d["c"], None, d["a"], None, d["b"], None, EPS], [d["x"]] + [None] * 5 + [d["a"], None, d["b"], None, EPS]]),
+        "linear_q8": (tvm.tvmattn_linear_jvp_fwd_q8, [
+            [e["xq"], e["xs"], e["txq"], e["txs"], e["wq"], e["ws"], b], [e["xq"], e["xs"], None, None, e["wq"], e["ws"]],
+            [e["xq"].view(2, 5, 64), e["xs"].view(2, 5), None, None, e["wq"], e["ws"], e["bias"], torch.float32]]),
+    }
+
+
+@pytest.mark.parametrize("name", ["rowquant", "gelu_q8", "gate_adaln_q8", "linear_q8"])
+def test_native_calls_against_the_python(monkeypatch, name):
+    from tests.test_fastcall import both
+    fn, calls = binding_calls()[name]
+    for a in calls:
+        both(monkeypatch, name, "native", fn, *a)
+    if name != "linear_q8":
+        fn, calls = binding_calls()[name]
+        a = [t.double() if isinstance(t, torch.Tensor) and t.dtype == torch.bfloat16 else t for t in calls[0]]
+        both(monkeypatch, name, "python", fn, *a)
+
+
+def refused(fn, *a, **kw):
+    with pytest.raises((ValueError, tvm.TvmattnError)):
+        fn(*a, **kw)
+
+
+def test_refusals():
+    q = tvm.tvmattn_rowquant_fwd
+    x = torch.randn(6, 64, device="cuda")
+    refused(q, x.half())
+    refused(q, x.expand(6, 64)[:1].expand(6, 64))        # rows that overlap
+    refused(q, x.t())
+    refused(q, x[:, 1:61])                               # misaligned
+    refused(q, x[:, :62])
+    refused(q, x, x[:, :32])
+    refused(q, x, x.bfloat16())
+    refused(q, x.view(2, 3, 64)[:, :, :32])              # a non-contiguous view of three dimensions
+    refused(q, torch.empty(0, 64, device="cuda"))
+    refused(q, torch.empty(4, 0, device="cuda"))
+    refused(q, x, out=(torch.empty(6, 64, dtype=torch.int8, device="cuda"), torch.empty(6, device="cuda"),
+                       torch.empty(6, 64, dtype=torch.int8, device="cuda"), torch.empty(6, device="cuda")))
+    refused(q, x, out=(torch.empty(6, 32, dtype=torch.int8, device="cuda"), torch.empty(6, device="cuda"), None, None))
+    t = {n: v.cuda() for n, v in norm_inputs(2, 3, 64, "bf16", 1).items()}
+    full = [t[n] for n in ORDER]
+    for n in range(10):                                  # each of them missing, each of them of another shape
+        refused(tvm.tvmattn_gate_adaln_jvp_fwd_q8, *full[:n], None, *full[n + 1:], EPS) if n else None
+        refused(tvm.tvmattn_gate_adaln_jvp_fwd_q8, *full[:n], full[n][:1], *full[n + 1:], EPS)
+    refused(tvm.tvmattn_gate_adaln_jvp_fwd_q8, *full, -1.0)
+    e = {n: v.cuda() for n, v in linear_inputs(6, 64, 40, 1).items()}
+    args = [e["xq"], e["xs"], e["txq"], e["txs"], e["wq"], e["ws"], e["bias"]]
+    f = lambda *a, **kw: tvm.tvmattn_linear_jvp_fwd_q8(*a, dtype=torch.float32, **kw)
+    for n in range(7):
+        refused(f, *args[:n], args[n].double(), *args[n + 1:])
+        refused(f, *args[:n], args[n][:-1], *args[n + 1:])
+    refused(f, *args[:2], None, *args[3:])
+    refused(f, *args[:3], None, *args[4:])
+    refused(tvm.tvmattn_linear_jvp_fwd_q8, *args, dtype=torch.float16)
+    refused(tvm.tvmattn_linear_jvp_fwd_q8, *args)        # a float32 bias with bfloat16 results
+    refused(f, *args, out=(torch.empty(6, 40, device="cuda"), None))
+    refused(f, *args, out=(torch.empty(5, 40, device="cuda"), torch.empty(5, 40, device="cuda")))
+    y = torch.empty(6, 40, device="cuda")
+    refused(f, *args, out=(y, y))
+
+
+def test_another_device_than_the_current_one_is_refused(monkeypatch):
+    x = torch.randn(6, 64, device="cuda")
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 1)
+    monkeypatch.setattr(tvm.binding, "_fast", tvm.binding._PythonOnly())
+    refused(tvm.tvmattn_rowquant_fwd, x)
+    refused(tvm.tvmattn_gate_adaln_jvp_fwd_q8, x.view(1, 6, 64), None, None, None, None, None, x[:1], None, x[:1], None, EPS)
+
+
+def test_results_do_not_depend_on_what_was_there_before():
+    """Every output element is written: outputs of a poisoned allocator pool against those of a clean one."""
+    t = norm_inputs(3, 33, 72, "bf16", 4)
+    e = {n: v.cuda() for n, v in linear_inputs(77, 144, 200, 5).items()}
+    def all_calls():
+        z = norm_call(t)
+        q = tvm.tvmattn_rowquant_fwd(t["x"].cuda(), t["tx"].cuda())
+        y = tvm.tvmattn_linear_jvp_fwd_q8(e["xq"], e["xs"], e["txq"], e["txs"], e["wq"], e["ws"])
+        return [r.clone() for r in (*z, *q, *y)]
+    first = all_calls()
+    for _ in range(3):
+        for n in (64, 1 << 10, 1 << 14, 1 << 16):
+            torch.full((n,), float("nan"), device="cuda")
+        for a, b in zip(all_calls(), first):
+            assert torch.equal(a, b)
