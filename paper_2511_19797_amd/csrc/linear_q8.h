@@ -16,12 +16,20 @@ __device__ __forceinline__ int lane_chunk(int wave, int lane) {
   return (pos & 7) ^ ((pos >> 4) & 7);
 }
 
-// Four consecutive floats or bf16 values as floats
-__device__ __forceinline__ f32x4 four(const float* p) { return *reinterpret_cast<const f32x4*>(p); }
-__device__ __forceinline__ f32x4 four(const bf16* p) {
-  const bf16x4 v = *reinterpret_cast<const bf16x4*>(p);
-  return f32x4{(float)v[0], (float)v[1], (float)v[2], (float)v[3]};
-}
+// Four consecutive floats or bf16 values: loaded as they are, bounds-checked (zeros beyond), and as floats.
+template <typename T>
+struct Four {
+  typedef __attribute__((ext_vector_type(sizeof(T)))) unsigned Raw;
+  Raw raw;
+  __device__ __forceinline__ void load(__amdgpu_buffer_rsrc_t rs, int at) {
+    if constexpr (sizeof(T) == 4) raw = __builtin_amdgcn_raw_buffer_load_b128(rs, at * 4, 0, 0);
+    else raw = __builtin_amdgcn_raw_buffer_load_b64(rs, at * 2, 0, 0);
+  }
+  __device__ __forceinline__ f32x4 values() const {
+    if constexpr (sizeof(T) == 4) return __builtin_bit_cast(f32x4, raw);
+    else return __builtin_bit_cast(f32x4, u32x4{raw[0] << 16, raw[0] & 0xffff0000u, raw[1] << 16, raw[1] & 0xffff0000u});
+  }
+};
 
 // The order of the output tiles (linear_gemm.h)
 struct TileOrder {

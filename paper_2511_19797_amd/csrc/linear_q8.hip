@@ -48,20 +48,26 @@ __global__ __launch_bounds__(256, OCC) void linear_q8_kernel(LinearQ8Args g, Til
   ox.setup(lds0, wi, wave, lane, pitchX);
   ow.setup(lds0 + HALF, wj, wave, lane, pitchW);
 
+  // Scales and biases (set 0 only), beyond the edges zeros.  As loaded: anything done to them here would make the compiler wait.
   float xs[W];
-  f32x4 ws[W][4], bias[W][4];
+  f32x4 ws[W][4];
+  Four<T> bias[W][4];
   {
-    const float* const from = second ? g.xs[1] : g.xs[0];
-    const bool biased = g.bias != nullptr && !second;
+    const __amdgpu_buffer_rsrc_t rx = __builtin_amdgcn_make_buffer_rsrc(const_cast<float*>(second ? g.xs[1] : g.xs[0]) + i0, 0,
+                                                                        min(g.R - i0, N) * 4, 0x00027000);
+    const __amdgpu_buffer_rsrc_t rw = __builtin_amdgcn_make_buffer_rsrc(const_cast<float*>(g.ws), 0, g.F * 4, 0x00027000);
+    const __amdgpu_buffer_rsrc_t rb = __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(g.bias), 0,
+                                                                        g.bias != nullptr && !second ? g.F * (int)sizeof(T) : 0, 0x00027000);
 #pragma unroll
-    for (int a = 0; a < W; ++a) xs[a] = from[min(i0 + (wi * W + a) * 32 + ic, g.R - 1)];
+    for (int a = 0; a < W; ++a)
+      xs[a] = __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(rx, ((wi * W + a) * 32 + ic) * 4, 0, 0));
 #pragma unroll
     for (int b = 0; b < W; ++b)
 #pragma unroll
       for (int q4 = 0; q4 < 4; ++q4) {
-        const int f = min(jw + b * 32 + 8 * q4 + 4 * hh, g.F - 4);  // (F is a multiple of 8: four channels are in range together)
-        ws[b][q4] = four(g.ws + f);
-        bias[b][q4] = biased ? four(static_cast<const T*>(g.bias) + f) : f32x4{0.f, 0.f, 0.f, 0.f};
+        const int f = jw + b * 32 + 8 * q4 + 4 * hh;
+        ws[b][q4] = __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(rw, f * 4, 0, 0));
+        bias[b][q4].load(rb, f);
       }
   }
 
@@ -143,6 +149,11 @@ __global__ __launch_bounds__(256, OCC) void linear_q8_kernel(LinearQ8Args g, Til
   __syncthreads();
   if (jw >= g.F) return;
   T* const y = static_cast<T*>(second ? g.y[1] : g.y[0]);
+  f32x4 bf[W][4];
+#pragma unroll
+  for (int b = 0; b < W; ++b)
+#pragma unroll
+    for (int q4 = 0; q4 < 4; ++q4) bf[b][q4] = bias[b][q4].values();
   const unsigned lw = lds0 + (unsigned)wave * OUT_REGION;
 #pragma unroll
   for (int a = 0; a < W; ++a) {
@@ -151,7 +162,7 @@ __global__ __launch_bounds__(256, OCC) void linear_q8_kernel(LinearQ8Args g, Til
 #pragma unroll
     for (int b = 0; b < W; ++b)
 #pragma unroll
-      for (int r = 0; r < 16; ++r) out[b][r] = fmaf((float)acc[a][b][r] * xs[a], ws[b][r >> 2][r & 3], bias[b][r >> 2][r & 3]);
+      for (int r = 0; r < 16; ++r) out[b][r] = fmaf((float)acc[a][b][r] * xs[a], ws[b][r >> 2][r & 3], bf[b][r >> 2][r & 3]);
     if constexpr (sizeof(T) == 2) {
       store_tile_coalesced<W>(lw, y + jw, g.ldy, i0 + (wi * W + a) * 32, g.R, g.F - jw, out, 1.f, lane);
     } else if (i < g.R) {

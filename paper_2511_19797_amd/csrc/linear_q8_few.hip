@@ -20,7 +20,7 @@ __device__ __forceinline__ void store_four(bf16* p, f32x4 v) {
 
 template <typename T, int NW>
 __global__ __launch_bounds__(64 * NW) void linear_q8_few_kernel(LinearQ8Args g, int rows) {
-  constexpr int U = 4;  // steps of 64 bytes in flight per wave
+  constexpr int U = 5;  // steps of 64 bytes in flight per wave
   __shared__ i32x4 part[NW][64];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int c = lane & 15, q = lane >> 4, f0 = blockIdx.x * 16;
@@ -30,6 +30,14 @@ __global__ __launch_bounds__(64 * NW) void linear_q8_few_kernel(LinearQ8Args g, 
   const bool first = s < g.R;
   const int r = first ? s : s - g.R;
   const signed char* const x = (first ? g.x[0] : g.x[1]) + (long long)r * g.ldx;
+  // scales and biases (not on the tangent) of what this lane ends up with, asked for first; beyond the edges zeros
+  const int f = f0 + 4 * q;
+  const float xs = (first ? g.xs[0] : g.xs[1])[r];
+  const f32x4 ws = __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(
+                                                 __builtin_amdgcn_make_buffer_rsrc(const_cast<float*>(g.ws), 0, g.F * 4, 0x00027000), f * 4, 0, 0));
+  Four<T> bias;
+  bias.load(__builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(g.bias), 0, g.bias != nullptr ? g.F * (int)sizeof(T) : 0, 0x00027000),
+            first ? f : g.F);
   i32x4 acc = {0, 0, 0, 0};
   const int steps = (g.K + 63) >> 6;
   for (int t0 = wave; t0 < steps; t0 += NW * U) {
@@ -41,20 +49,19 @@ __global__ __launch_bounds__(64 * NW) void linear_q8_few_kernel(LinearQ8Args g, 
       w[u] = __builtin_bit_cast(i32x4, __builtin_amdgcn_raw_buffer_load_b128(rw, in ? c * g.K + k : (int)kNowhere, 0, 0));
       xv[u] = *reinterpret_cast<const i32x4*>(x + (in ? k : 0));
     }
+    __builtin_amdgcn_sched_barrier(0);  // all loads first
 #pragma unroll
     for (int u = 0; u < U; ++u) acc = __builtin_amdgcn_mfma_i32_16x16x64_i8(w[u], xv[u], acc, 0, 0, 0);
   }
   part[wave][lane] = acc;
   __syncthreads();
-  const int f = f0 + 4 * q;
   if (wave != 0 || c >= rows || f >= g.F) return;  // (F is a multiple of 8: four channels are in range together)
 #pragma unroll
   for (int w = 1; w < NW; ++w) acc += part[w][lane];
-  const float xs = (first ? g.xs[0] : g.xs[1])[r];
-  const f32x4 ws = four(g.ws + f), bias = first && g.bias != nullptr ? four(static_cast<const T*>(g.bias) + f) : f32x4{0.f, 0.f, 0.f, 0.f};
+  const f32x4 b4 = bias.values();
   f32x4 o;
 #pragma unroll
-  for (int e = 0; e < 4; ++e) o[e] = fmaf((float)acc[e] * xs, ws[e], bias[e]);
+  for (int e = 0; e < 4; ++e) o[e] = fmaf((float)acc[e] * xs, ws[e], b4[e]);
   store_four(static_cast<T*>(first ? g.y[0] : g.y[1]) + (long long)r * g.ldy + f, o);
 }
 
