@@ -744,9 +744,9 @@ def tvmattn_linear_jvp_fwd_q8(xq, xs, txq, txs, wq, ws, bias=None, dtype=torch.b
     """Returns (y, ty): the linear layer of 8-bit rows xq ([..., K] int8, or 2-D [R, K] views with a row pitch) with scales xs [...]
     and an 8-bit weight wq [F, K] with scales ws [F], in `dtype` (bfloat16 or float32, the bias's too).  txq, txs None: no tangent,
     ty is None.  `out`: preallocated (y, ty), contiguous [..., F] or 2-D [R, F] views with a row pitch."""
-    if out is None:
-        r = (_fast or _load_fast()).linear_q8(xq, xs, txq, txs, wq, ws, bias, dtype is torch.bfloat16 if dtype in
-                                              (torch.bfloat16, torch.float32) else None)
+    half = dtype is torch.bfloat16
+    if out is None and (half or dtype is torch.float32):
+        r = (_fast or _load_fast()).linear_q8(xq, xs, txq, txs, wq, ws, bias, half)
         if r is not None:
             return _taken(r)
     if wq.dim() != 2 or wq.dtype != torch.int8 or not wq.is_contiguous() or wq.device != xq.device:

@@ -277,7 +277,9 @@ __global__ __launch_bounds__(256, 1) void q8_pipe_kernel(LinearQ8Args g, TileOrd
         const bool swapped = !WIDE && it >= (wide ? 2 : 1);
         const u32x4 o = swapped ? u32x4{v[it][2], v[it][3], v[it][0], v[it][1]} : v[it];
         const unsigned off = (wide ? out128 : out64) + (unsigned)(a * 32 + it * (wide ? 8 : 16)) * pitch + (unsigned)(b0 * 32 * E);
-        __builtin_amdgcn_raw_buffer_store_b128(o, rs, (int)(in ? off : kNowhere), 0, 0);
+        // (streamed past the L2, sc1 nt, which is the operands': a block of 16 x 1024 tokens 1112 to 1094 us, 1152 -> 4608 on
+        // buffers that change from call to call 202 to 191; with nt alone 1152 -> 3456 takes 159 us instead of 142)
+        __builtin_amdgcn_raw_buffer_store_b128(o, rs, (int)(in ? off : kNowhere), 0, 18);
       }
     };
     park(0);
