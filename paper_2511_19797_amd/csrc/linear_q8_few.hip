@@ -5,9 +5,9 @@
 // into fragments (16 rows x 64 bytes of the weight per load: whole 64-byte segments, no LDS), several loads in flight, and add
 // their exact integer sums in LDS.  v_mfma_i32_16x16x64_i8, D = W-fragment x X-fragment: a lane ends up with four consecutive
 // channels of one row.
-// One row, K = 1152, F = 6912: 3.9 us from the caches, 4.7 - 5.6 us from memory (8 MB), of which an empty launch is 2; on 64 x 64
-// tiles 5.3.  K = 4608, F = 1152: 5.0 and 5.4 against 11.1.  From 17 rows on the tiles are as fast (32 rows, K = 1152: 5.0 against 5.8
-// here, every workgroup reading all rows).
+// One row, K = 1152, F = 6912: 3.8 us from the caches, 4.7 from memory (8 MB), of which an empty launch is 1.4; on 64 x 64 tiles 5.3.
+// K = 4608, F = 1152: 4.7 and 4.6 against 11.1.  Sixteen rows, F = 6912: 4.5 against 5.4.  From 17 rows on the tiles are as fast (32 rows,
+// K = 1152: 5.0 against 5.8 here, every workgroup reading all rows).
 #include "linear_q8.h"
 
 namespace tvm {

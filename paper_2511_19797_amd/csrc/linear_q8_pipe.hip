@@ -8,6 +8,11 @@
 // as row broadcasts (a data-parallel-primitive operand): two registers per block instead of 32.  They come by asynchronous loads
 // into LDS, asked for when the output tile begins: with loads into registers the compiler waited, at the tile's end, for every
 // load in flight.
+// us (POP/s), bf16 results: 2 x 16384 x 1152 -> 3456 141 (1.85), -> 1152 51 (1.7), -> 4608 180 - 200 (1.9), 2 x 16384 x 4608 -> 1152 147 (2.35),
+// 8192 x 4608 -> 1152 42 (2.1); on 128 x 128 tiles 241, 82, 324, 219, 71.  What bounds it is power: at 2.35 POP/s the clock is 1.75 GHz with the
+// matrix cores 64 % busy, and changes that save cycles (the barrier's slot, the order of fragment reads, of tiles) leave the times
+// as they are.  At K = 1152 an output tile's end is a third of its cycles, 12 k of 30 k; 256 x 256 tiles are no faster there
+// (146 against 144 at -> 3456) and lose where they do not divide the layer (167 against 148 at 4608 -> 1152).
 #include <type_traits>
 
 #include "linear_gemm.h"
@@ -25,8 +30,8 @@ __device__ __forceinline__ void mfma_acc_q8(i32x16& acc, bf16x8 a, bf16x8 b) {
 }
 // Eight results of a block: registers 8 H ... 8 H + 7 of its sums, times the token's scale, times the channels' scales, plus their
 // biases.  (Assembly: the compiler would broadcast every channel's scale and bias once and keep them all, in registers it does not
-// have.  The eight reads
-// in front are more than the two slots due between a register copy that it may put there and the broadcasts that read the copy.)
+// have.  The eight reads in front are more than the two slots due between a register copy that it may put there and the broadcasts
+// that read the copy.)
 template <int H>
 __device__ __forceinline__ void results(float (&v)[8], const i32x16& t, float xs, float ws, float bias) {
   float u[8];

@@ -209,6 +209,28 @@ def test_gate_adaln_rows_stay_by_themselves():
         assert torch.equal(a[keep], b[keep])
 
 
+def test_gate_adaln_with_a_modulation_that_is_not_finite():
+    """z is NaN where the two separate operators make it so, and nowhere else; rows that take such a vector are NaN."""
+    for at, v in ((1151, float("inf")), (3, float("-inf")), (700, float("nan"))):
+        t = norm_inputs(2, 6, 1152, "bf16", 11)
+        t["c"][1, at] = v
+        z, tz, q, s, tq, ts = norm_call(t)
+        ref, tref = tvm.tvmattn_gate_jvp_fwd(*(t[n].cuda() for n in ("x", "tx", "h", "th", "c", "tc")), EPS)
+        assert torch.equal(torch.isnan(z), torch.isnan(ref)) and torch.equal(torch.isnan(tz), torch.isnan(tref))
+        assert torch.isnan(s[1]).all() and not q[1].any() and torch.isfinite(s[0]).all() and torch.isfinite(z[0]).all()
+
+
+def test_gate_adaln_against_the_two_operators():
+    """z and the modulated tokens of the bf16 operators: z to one rounding, the 8-bit rows to half a step and the roundings between."""
+    t = {n: v.cuda() for n, v in norm_inputs(4, 100, 1152, "bf16", 12).items()}
+    z, tz, q, s, tq, ts = norm_call(t)
+    rz, rtz = tvm.tvmattn_gate_jvp_fwd(*(t[n] for n in ORDER[:6]), EPS)
+    y, ty = tvm.tvmattn_adaln_jvp_fwd(rz, rtz, *(t[n] for n in ORDER[6:]), EPS)
+    assert torch.allclose(z.float(), rz.float(), rtol=2 ** -7, atol=1e-6) and torch.allclose(tz.float(), rtz.float(), rtol=2 ** -7, atol=1e-5)
+    for r, k, v in ((q, s, y), (tq, ts, ty)):
+        assert ((r.float() * k.unsqueeze(-1) - v.float()).abs() <= 0.5 * k.unsqueeze(-1) + 2 ** -6 * v.float().abs().amax(-1, keepdim=True)).all()
+
+
 # ---- the linear layer
 LINEAR = [
     (1, 16, 8), (1, 1152, 6912), (2, 48, 40), (7, 4608, 1152), (16, 1152, 1160), (17, 1168, 72), (33, 32, 8),
