@@ -23,7 +23,7 @@ namespace {
 
 constexpr int kWI = 4;              // 32-row blocks of a wave
 constexpr unsigned kXTile = 32768;  // LDS: three X tiles, then two W tiles
-constexpr unsigned kScales = 3072;
+constexpr unsigned kScales = 3 * 1024;
 
 __device__ __forceinline__ void mfma_acc_q8(i32x16& acc, bf16x8 a, bf16x8 b) {
   asm volatile("v_mfma_i32_32x32x32_i8 %0, %1, %2, %0" : "+a"(acc) : "v"(a), "v"(b));

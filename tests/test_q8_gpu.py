@@ -465,3 +465,58 @@ def test_results_do_not_depend_on_what_was_there_before():
             torch.full((n,), float("nan"), device="cuda")
         for a, b in zip(all_calls(), first):
             assert torch.equal(a, b)
+
+
+# ---- offsets past 32 bits: the last rows of a wide or long buffer as in a small call, bit for bit
+def test_wide_pitches():
+    rng = np.random.default_rng(6)
+    x = draw(rng, 40, 64, dtype="bf16").cuda()
+    buf = torch.empty(70000, 65536, dtype=torch.bfloat16, device="cuda")          # 9 GB
+    buf[:, :64] = 0
+    buf[-40:, :64] = x
+    for fn in (tvm.tvmattn_rowquant_fwd, tvm.tvmattn_gelu_jvp_fwd_q8):
+        q, s, _, _ = fn(buf[:, :64])
+        rq, rs, _, _ = fn(x)
+        assert torch.equal(q[-40:], rq) and torch.equal(s[-40:], rs) and not q[:-40].any() and not s[:-40].any()
+    del buf
+
+
+@pytest.mark.parametrize("K,F", [(64, 1152), (144, 72)])
+def test_linear_with_wide_pitches(K, F):
+    R, keep, wide = 5000, 300, 1 << 20
+    t = {n: v.cuda() for n, v in linear_inputs(keep, K, F, 8).items()}
+    xq = torch.empty(R, wide, dtype=torch.int8, device="cuda")                    # 5 GB
+    xq[:, :K] = 0
+    xq[-keep:, :K] = t["xq"]
+    xs = torch.ones(R, device="cuda")
+    xs[-keep:] = t["xs"]
+    y = torch.empty(R, wide, dtype=torch.bfloat16, device="cuda")                 # 10 GB
+    y[:, F] = 3.0
+    bias = t["bias"].bfloat16()
+    tvm.tvmattn_linear_jvp_fwd_q8(xq[:, :K], xs, None, None, t["wq"], t["ws"], bias, out=(y[:, :F], None))
+    ref, _ = tvm.tvmattn_linear_jvp_fwd_q8(t["xq"], t["xs"], None, None, t["wq"], t["ws"], bias)
+    assert torch.equal(y[-keep:, :F], ref) and (y[:-keep, :F] == bias).all() and (y[:, F] == 3.0).all()
+
+
+def test_long_streams():
+    B, T, C = 17, 65536, 2048                                                     # 2.3 G values: 4.6 GB a tensor
+    t = norm_inputs(1, 30, C, "bf16", 13)
+    x, h = (torch.zeros(B, T, C, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    x[-1, -30:], h[-1, -30:] = t["x"][0].cuda(), t["h"][0].cuda()
+    mods = [torch.ones(B, C, device="cuda") for _ in range(3)]
+    for m, n in zip(mods, ("c", "a", "b")):
+        m[-1] = t[n][0].cuda()
+    z, _, q, s, _, _ = tvm.tvmattn_gate_adaln_jvp_fwd_q8(x, None, h, None, mods[0], None, mods[1], None, mods[2], None, EPS)
+    rz, _, rq, rs, _, _ = norm_call(t, True, False)
+    assert torch.equal(z[-1, -30:], rz[0]) and torch.equal(q[-1, -30:], rq[0]) and torch.equal(s[-1, -30:], rs[0])
+    assert (q[0, ::997] == 127).all() and not z[0, ::997].any()                   # rows of zeros: y is the shift, all ones
+
+
+def test_many_rows():
+    """More workgroups than one dimension of a launch holds."""
+    R = (1 << 22) + 9
+    x = torch.zeros(R, 8, dtype=torch.bfloat16, device="cuda")
+    x[-3:] = torch.arange(24, device="cuda").view(3, 8).bfloat16()
+    q, s, _, _ = tvm.tvmattn_rowquant_fwd(x)
+    check_rows(q[-3:], s[-3:], x[-3:].double().cpu().numpy())
+    assert not q[:-3].any() and not s[:-3].any()
