@@ -35,18 +35,16 @@ struct Four {
 struct TileOrder {
   int sets;
   Divisor by_set, by_group, by_rest;
+  bool stream;  // (256-row tiles: how results are stored)
 };
 inline TileOrder tile_order(int shape, int sets, int R, int F) {
-  GemmArgs g{};
-  g.I = R;
-  g.J = F;
-  g.set_divisors(shape, false);
-  return TileOrder{sets, g.by_set, g.by_group, g.by_rest};
+  const long long nI = ((long long)R + kTileRowsQ8[shape] - 1) / kTileRowsQ8[shape], nJ = ((long long)F + kTileColsQ8[shape] - 1) / kTileColsQ8[shape];
+  return TileOrder{sets, Divisor::of((unsigned)(nI * nJ)), Divisor::of((unsigned)(kGI * nJ)), Divisor::of(nI % kGI == 0 ? 1u : (unsigned)(nI % kGI)), false};
 }
 
 // A handful of rows (linear_q8_few.hip).
 hipError_t launch_linear_q8_few(const LinearQ8Args& a, int dtype, hipStream_t st);
-// 256 x 192 tiles (linear_q8_pipe.hip).
-hipError_t launch_linear_q8_pipe(const LinearQ8Args& a, int dtype, hipStream_t st);
+// The 256-row tile shapes (linear_q8_pipe.hip).
+hipError_t launch_linear_q8_pipe(int shape, const LinearQ8Args& a, int dtype, hipStream_t st);
 
 }  // namespace tvm

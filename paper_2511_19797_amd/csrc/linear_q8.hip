@@ -184,9 +184,9 @@ __global__ __launch_bounds__(256, OCC) void linear_q8_kernel(LinearQ8Args g, Til
 template <typename T>
 hipError_t launch_tiles(int shape, const LinearQ8Args& a, hipStream_t st) {
   const int sets = a.x[1] != nullptr ? 2 : 1;
-  const dim3 grid((unsigned)small_workgroups(sets * tiles_of(shape, a.R, a.F))), block(kSmallThreads);
+  const dim3 grid((unsigned)small_workgroups(sets * tiles_q8(shape, a.R, a.F))), block(kSmallThreads);
   const TileOrder order = tile_order(shape, sets, a.R, a.F);
-  if (shape == k128) hipLaunchKernelGGL((linear_q8_kernel<T, 128, 4, 1>), grid, block, 0, st, a, order);
+  if (shape == kQ128) hipLaunchKernelGGL((linear_q8_kernel<T, 128, 4, 1>), grid, block, 0, st, a, order);
   else hipLaunchKernelGGL((linear_q8_kernel<T, 64, 5, 2>), grid, block, 0, st, a, order);
   return hipGetLastError();
 }
@@ -197,7 +197,7 @@ hipError_t launch_linear_q8(const LinearQ8Args& a, int dtype, hipStream_t st) {
   const int sets = a.x[1] != nullptr ? 2 : 1;
   if ((long long)sets * a.R <= kFewRows) return launch_linear_q8_few(a, dtype, st);
   const int shape = pick_shape_q8(sets, a.R, a.F, a.K);
-  if (shape == k192) return launch_linear_q8_pipe(a, dtype, st);
+  if (shape <= kQ256x128) return launch_linear_q8_pipe(shape, a, dtype, st);
   return dtype == 1 ? launch_tiles<bf16>(shape, a, st) : launch_tiles<float>(shape, a, st);
 }
 

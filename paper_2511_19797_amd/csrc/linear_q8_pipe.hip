@@ -1,18 +1,19 @@
-// The 8-bit linear layers (linear_q8.hip) on 256 x 192 output tiles, hand-scheduled like the bf16 ones
+// The 8-bit linear layers (linear_q8.hip) on 256 x 192 and 256 x 128 output tiles, hand-scheduled like the bf16 ones
 // (linear_pipe.hip, whose layout of LDS, fragment reads and loads this is: 128 bytes of a row per contraction tile, here 128 entries).
 //
-// Four waves, one per SIMD, as 2 x 2, each with 4 x 3 blocks of 32 x 32 in AGPRs; three X tiles and two W tiles in LDS; the
+// Four waves, one per SIMD, as 2 x 2, each with 4 x 3 (4 x 2) blocks of 32 x 32 in AGPRs; three X tiles and two W tiles in LDS; the
 // fragments of two contraction steps ahead are read between the products, the loads of later tiles in the slots between.
 // Results: a lane owns a token and 16 channels of a block.  The token's scale is a register per block row.  A channel's scale and
 // bias belong to a register index, so every row of 16 lanes holds the 16 of its half, one per lane, and the arithmetic takes them
 // as row broadcasts (a data-parallel-primitive operand): two registers per block instead of 32.  They come by asynchronous loads
 // into LDS, asked for when the output tile begins: with loads into registers the compiler waited, at the tile's end, for every
 // load in flight.
-// us (POP/s), bf16 results: 2 x 16384 x 1152 -> 3456 141 (1.85), -> 1152 51 (1.7), -> 4608 180 - 200 (1.9), 2 x 16384 x 4608 -> 1152 147 (2.35),
-// 8192 x 4608 -> 1152 42 (2.1); on 128 x 128 tiles 241, 82, 324, 219, 71.  What bounds it is power: at 2.35 POP/s the clock is 1.75 GHz with the
-// matrix cores 64 % busy, and changes that save cycles (the barrier's slot, the order of fragment reads, of tiles) leave the times
-// as they are.  At K = 1152 an output tile's end is a third of its cycles, 12 k of 30 k; 256 x 256 tiles are no faster there
-// (146 against 144 at -> 3456) and lose where they do not divide the layer (167 against 148 at 4608 -> 1152).
+// us (POP/s) on 256 x 192, bf16 results: 2 x 16384 x 1152 -> 3456 146 (1.8), -> 1152 52 (1.7), -> 4608 188 (1.85), 2 x 16384 x 4608 -> 1152
+// 145 (2.4), 8192 x 4608 -> 1152 42 (2.1); float32 results, 1152 -> 3456 162; on 128 x 128 tiles 213, 76, 293, 213, 67; 260.  What bounds it is
+// power: at 2.4 POP/s the clock is 1.75 GHz with the matrix cores 64 % busy, and changes that save cycles (the barrier's slot, the
+// order of fragment reads, of tiles) leave the times as they are.  At K = 1152 an output tile's end is a third of its cycles, 12 k of 30 k;
+// 256 x 256 tiles are no faster there (146 against 144 at -> 3456) and lose where they do not divide the layer (167 against 148
+// at 4608 -> 1152).  256 x 128 is for shapes whose tiles it deals out better: 2 x 1000 x 1152 -> 3456 12.1 us, 14.4 on 256 x 192.
 #include <type_traits>
 
 #include "linear_gemm.h"
@@ -24,6 +25,11 @@ namespace {
 constexpr int kWI = 4;              // 32-row blocks of a wave
 constexpr unsigned kXTile = 32768;  // LDS: three X tiles, then two W tiles
 constexpr unsigned kScales = 3 * 1024;
+// Results whose rows are whole 64-byte pieces of memory are streamed past the L2 (sc1 nt), which then is the operands': us without | with,
+// 2 x 16384 x 1152 -> 4608 on buffers that change from call to call 189 | 175, on the same ones 184 | 185, 4619 x 624 -> 5376 31.2 |
+// 30.6, float32 2 x 16384 x 1152 -> 3456 166 | 155.  Where pieces of rows share their 64 bytes, every one of them goes to
+// memory twice: 2 x 5103 x 192 -> 6408 47 | 114.
+constexpr int kStreamed = 18;
 
 __device__ __forceinline__ void mfma_acc_q8(i32x16& acc, bf16x8 a, bf16x8 b) {
   asm volatile("v_mfma_i32_32x32x32_i8 %0, %1, %2, %0" : "+a"(acc) : "v"(a), "v"(b));
@@ -87,9 +93,9 @@ __device__ __forceinline__ void load_lds4(u32x4 srd, unsigned voff, unsigned lds
   asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dword %1, %2, 0 offen lds" ::"s"(lds), "v"(voff), "s"(srd) : "memory", "m0");
 }
 
-template <typename T>
+template <typename T, int WJ>
 __global__ __launch_bounds__(256, 1) void q8_pipe_kernel(LinearQ8Args g, TileOrder order) {
-  constexpr int kTI = 256, WJ = 3, kTJ = 64 * WJ;
+  constexpr int kTI = 256, kTJ = 64 * WJ;
   constexpr unsigned kWTile = kTJ * 128u;
   constexpr bool WIDE = sizeof(T) == 4;        // float32 results
   using OX = Operand<false, kTI>;
@@ -282,9 +288,8 @@ __global__ __launch_bounds__(256, 1) void q8_pipe_kernel(LinearQ8Args g, TileOrd
         const bool swapped = !WIDE && it >= (wide ? 2 : 1);
         const u32x4 o = swapped ? u32x4{v[it][2], v[it][3], v[it][0], v[it][1]} : v[it];
         const unsigned off = (wide ? out128 : out64) + (unsigned)(a * 32 + it * (wide ? 8 : 16)) * pitch + (unsigned)(b0 * 32 * E);
-        // (streamed past the L2, sc1 nt, which is the operands': a block of 16 x 1024 tokens 1112 to 1094 us, 1152 -> 4608 on
-        // buffers that change from call to call 202 to 191; with nt alone 1152 -> 3456 takes 159 us instead of 142)
-        __builtin_amdgcn_raw_buffer_store_b128(o, rs, (int)(in ? off : kNowhere), 0, 18);
+        if (order.stream) __builtin_amdgcn_raw_buffer_store_b128(o, rs, (int)(in ? off : kNowhere), 0, kStreamed);
+        else __builtin_amdgcn_raw_buffer_store_b128(o, rs, (int)(in ? off : kNowhere), 0, 0);
       }
     };
     park(0);
@@ -370,8 +375,10 @@ __global__ __launch_bounds__(256, 1) void q8_pipe_kernel(LinearQ8Args g, TileOrd
           x_next = x_free;
           fresh = 0;
         }
+        // (the descriptors move behind the tile's last loads: at the very end they are of size 0, which the move lets wrap)
+        static_assert(kk != 3 || slots.at[(L - 1) * nfree / L] <= NP - 1, "W loads in front of their descriptor's move");
         if (kk == 3 && m == NP / 2) further_x();
-        if (kk == 3 && m == NP - 2) {
+        if (kk == 3 && m == NP - 1) {
           slot_w += w_step;
           w_step = 0u - w_step;
           further_w();
@@ -412,19 +419,22 @@ __global__ __launch_bounds__(256, 1) void q8_pipe_kernel(LinearQ8Args g, TileOrd
 }
 
 template <typename T>
-hipError_t launch(const LinearQ8Args& a, hipStream_t st) {
+hipError_t launch(int shape, const LinearQ8Args& a, hipStream_t st) {
   const int sets = a.x[1] != nullptr ? 2 : 1;
-  const long long tiles = sets * tiles_of(k192, a.R, a.F), per = (tiles + 7) / 8;
+  const long long tiles = sets * tiles_q8(shape, a.R, a.F), per = (tiles + 7) / 8;
   const dim3 grid((unsigned)(8 * (per < 32 ? per : 32)));  // 8 XCDs x at most 32 CUs, fewer where an XCD's share of the tiles is smaller
-  hipLaunchKernelGGL((q8_pipe_kernel<T>), grid, dim3(256), 0, st, a, tile_order(k192, sets, a.R, a.F));
+  TileOrder order = tile_order(shape, sets, a.R, a.F);
+  order.stream = ((a.ldy * (long long)sizeof(T)) | (long long)(reinterpret_cast<uintptr_t>(a.y[0]) | reinterpret_cast<uintptr_t>(a.y[1]))) % 64 == 0;
+  if (shape == kQ256x192) hipLaunchKernelGGL((q8_pipe_kernel<T, 3>), grid, dim3(256), 0, st, a, order);
+  else hipLaunchKernelGGL((q8_pipe_kernel<T, 2>), grid, dim3(256), 0, st, a, order);
   return hipGetLastError();
 }
-static_assert(kTileI[k192] == 256 && kTileJ[k192] == 192, "the plan's tiles");
+static_assert(kTileColsQ8[kQ256x192] == 64 * 3 && kTileColsQ8[kQ256x128] == 64 * 2, "the plan's tiles");
 
 }  // namespace
 
-hipError_t launch_linear_q8_pipe(const LinearQ8Args& a, int dtype, hipStream_t st) {
-  return dtype == 1 ? launch<bf16>(a, st) : launch<float>(a, st);
+hipError_t launch_linear_q8_pipe(int shape, const LinearQ8Args& a, int dtype, hipStream_t st) {
+  return dtype == 1 ? launch<bf16>(shape, a, st) : launch<float>(shape, a, st);
 }
 
 }  // namespace tvm

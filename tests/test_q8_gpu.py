@@ -237,6 +237,7 @@ LINEAR = [
     (64, 128, 64), (65, 144, 72), (250, 768, 2304), (256, 1152, 1152), (500, 400, 1000), (129, 112, 136),
     (300, 4624, 264), (1000, 1152, 3456), (1030, 2320, 520), (2100, 64, 2056), (4000, 1152, 1152), (70, 65536, 16),
     (9000, 64, 1160), (9000, 112, 1160), (9000, 208, 1160),   # several output tiles per workgroup, of one and two contraction tiles
+    (1000, 1168, 3456), (600, 1024, 5000), (530, 2048, 3480),  # 256 x 128 tiles, rows in 64-byte pieces and not
     (9, 1152, 40), (8, 2064, 1160), (16, 4608, 200),           # a handful of rows, two sets of them and one; 4 waves and 8
 ]
 

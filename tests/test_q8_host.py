@@ -100,10 +100,12 @@ def test_host_code_under_asan_and_ubsan(tmp_path):
 
 def test_tile_shapes():
     """The measured sides of the rule's borders, and that a launch can hold what is chosen."""
-    cases = {(1, 64, 1152, 4608): 64, (2, 256, 1152, 1152): 64, (2, 642, 2248, 4528): 128, (2, 1000, 3456, 1152): 256, (2, 4096, 1152, 1152): 256,
-             (2, 16384, 3456, 1152): 256, (1, 8192, 1152, 4608): 256, (1, 17, 8, 16): 64, (2, 1 << 30, 8, 16): 256, (1, 1 << 18, 1 << 20, 16): 256}
+    cases = {(1, 64, 1152, 4608): (64, 64), (2, 256, 1152, 1152): (64, 64), (1, 512, 4608, 1152): (128, 128), (2, 642, 2248, 4528): (128, 128),
+             (2, 1000, 3456, 1152): (256, 128), (2, 4096, 1152, 1152): (256, 192), (2, 16384, 3456, 1152): (256, 192),
+             (1, 8192, 1152, 4608): (256, 192), (1, 17, 8, 16): (64, 64), (2, 1 << 30, 8, 16): (256, 128), (1, 1 << 18, 1 << 20, 16): (256, 128)}
     src = '#include "linear_q8_plan.h"\n#include <cstdio>\nint main(){int s,R,F,K; while(std::scanf("%d %d %d %d",&s,&R,&F,&K)==4)' \
-          '{int n=tvm::pick_shape_q8(s,R,F,K); std::printf("%d %d\\n",tvm::kTileI[n],(int)tvm::grid_fits(n,s*tvm::tiles_of(n,R,F)));}}'
+          '{int n=tvm::pick_shape_q8(s,R,F,K); long long t=s*tvm::tiles_q8(n,R,F);' \
+          'std::printf("%d %d %d\\n",tvm::kTileRowsQ8[n],tvm::kTileColsQ8[n],(int)(tvm::grid_fits_q8(n,t)&&t<(1ll<<31)));}}'
     with tempfile.TemporaryDirectory() as tmp:
         open(os.path.join(tmp, "p.cpp"), "w").write(src)
         exe = os.path.join(tmp, "p")
@@ -112,7 +114,7 @@ def test_tile_shapes():
         assert r.returncode == 0, r.stderr
         r = subprocess.run([exe], input="\n".join(" ".join(map(str, c)) for c in cases), capture_output=True, text=True)
     assert r.returncode == 0, r.stderr
-    assert [tuple(map(int, l.split())) for l in r.stdout.splitlines()] == [(rows, 1) for rows in cases.values()]
+    assert [tuple(map(int, l.split())) for l in r.stdout.splitlines()] == [(*tile, 1) for tile in cases.values()]
 
 
 def broadcast_violations(asm_text):
@@ -140,7 +142,7 @@ def test_broadcast_check_sees_a_planted_hazard():
 def test_instruction_streams():
     """The rules that no interlock keeps, in the hand-scheduled kernel; the loads into LDS in the small tiles' too; nothing spills."""
     text = generated("linear_q8_pipe.hip")
-    assert text.count("v_mfma_i32") > 2 * 48 and text.count("offen lds") > 60 and text.count("row_newbcast") > 300
+    assert text.count("v_mfma_i32") > 2 * (48 + 32) and text.count("offen lds") > 60 and text.count("row_newbcast") > 300
     assert isa.violations(text) == [] and isa.result_violations(text) == [] and broadcast_violations(text) == []
     for name in ("linear_q8_pipe.hip", "linear_q8.hip"):
         text = generated(name)
