@@ -6,7 +6,7 @@
 // A row belongs to one wave where it fits (4 chunks of 16 bytes per lane: 2048 bf16 values), so that its maximum and its sums
 // are lane exchanges, with no barrier; longer rows belong to 4 or 16 waves, which meet once in LDS.
 // us (TB/s of what has to be read and written): rows of 16384 x 1152 with tangent, bf16, 19.6 (5.8); activation 16384 x 4608 with tangent 76.7
-// (5.9), 250 x 1536 float32 2.7; norm with residual and tangent 16 x 1024 x 1152 50.5 (5.2), 1 x 256 x 1152 6.3.
+// (5.9), 250 x 1536 float32 2.7; norm with residual and tangent 16 x 1024 x 1152 50.5 (5.2), 1 x 256 x 1152 6.4.
 #include <algorithm>
 
 #include "gelu_math.h"
@@ -132,7 +132,7 @@ __global__ __launch_bounds__(NW == 1 ? 256 : 64 * NW) void rows_q8_kernel(RowsQ8
 // into LDS (with the tangents 24 bytes per column), and its four waves then take a row each, with no further barrier.  120 registers
 // at three chunks per lane, four waves per SIMD: with a row's chunks interleaved and the next row's on their way it took 256, and 71 us
 // instead of 50 at 16 x 1024 x 1152.
-constexpr int kNormWaves = 4;
+constexpr int kNormWaves = 4;  // (2 | 4 | 8: 16 x 1024 x 1152 118 | 50 | 52 us, 1 x 256 x 1152 8.3 | 6.4 | 7.2)
 template <typename T, bool TAN, bool GATE, int NCH>
 __global__ __launch_bounds__(64 * kNormWaves, NCH <= 3 ? 4 : NCH == 4 ? 3 : 1) void gate_adaln_q8_kernel(GateAdalnQ8Args g) {
   constexpr int VEC = Chunk<T>::VEC, NV = GATE ? 3 : 2, PL = VEC / 4;
@@ -144,7 +144,7 @@ __global__ __launch_bounds__(64 * kNormWaves, NCH <= 3 ? 4 : NCH == 4 ? 3 : 1) v
   const long long base = (long long)b * g.T;
   const T *x = static_cast<const T*>(g.x), *tx = static_cast<const T*>(g.tx), *h = static_cast<const T*>(g.h), *th = static_cast<const T*>(g.th);
   Raw<T> rx[NCH], rh[GATE ? NCH : 1], rt[TAN ? NCH : 1], rth[TAN && GATE ? NCH : 1];
-  auto load = [&](int t) {
+  auto load = [&](unsigned t) {
     const long long at0 = (base + t) * g.C;
 #pragma unroll
     for (int j = 0; j < NCH; ++j) {  // chunks past the row's end are read as the first one and take no further part
@@ -156,7 +156,8 @@ __global__ __launch_bounds__(64 * kNormWaves, NCH <= 3 ? 4 : NCH == 4 ? 3 : 1) v
       if constexpr (TAN && GATE) rth[j] = load_raw<T>(th + at);
     }
   };
-  int t = blockIdx.x * kNormWaves + wave;
+  unsigned t = blockIdx.x * kNormWaves + (unsigned)wave;  // (T < 2^31: a step past the last row stays in range)
+  const unsigned T_rows = (unsigned)g.T;
   // Where quad n (four columns) of a vector is kept; this thread's quads are tid + 256 i.  All loads first, the first row's behind
   // them: the prologue is one memory latency and two barriers.
   constexpr int NQ = (NCH * PL + 3) / 4, NT = 64 * kNormWaves;
@@ -172,7 +173,7 @@ __global__ __launch_bounds__(64 * kNormWaves, NCH <= 3 ? 4 : NCH == 4 ? 3 : 1) v
       v4[k][i] = *reinterpret_cast<const float4*>(vs[k] + at);
       if constexpr (TAN) t4[k][i] = *reinterpret_cast<const float4*>(tvs[k] + at);
     }
-  if (t < g.T) load(t);
+  if (t < T_rows) load(t);
   __builtin_amdgcn_sched_barrier(0);
   float sums[2 * NV];
 #pragma unroll
@@ -229,7 +230,7 @@ __global__ __launch_bounds__(64 * kNormWaves, NCH <= 3 ? 4 : NCH == 4 ? 3 : 1) v
     }
   };
   constexpr int A = 0, TA = 1, B = TAN ? 2 : 1, TB = 3, C = TAN ? 4 : 2, TC = 5;
-  while (t < g.T) {
+  while (t < T_rows) {
     const long long row = base + t, at0 = row * g.C;
     float v[NCH][VEC], w[TAN ? NCH : 1][VEC];
     float sxx = 0.f, sxt = 0.f;
@@ -306,7 +307,7 @@ __global__ __launch_bounds__(64 * kNormWaves, NCH <= 3 ? 4 : NCH == 4 ? 3 : 1) v
       }
     }
     t += gridDim.x * kNormWaves;
-    if (t < g.T) load(t);
+    if (t < T_rows) load(t);
   }
 }
 
@@ -329,7 +330,7 @@ template <typename T, bool TAN, bool GATE>
 hipError_t launch_norm(const GateAdalnQ8Args& a, hipStream_t st) {
   const int chunks = a.C / Chunk<T>::VEC, NCH = (chunks + 63) / 64;
   // about 1024 workgroups in all, and every one of a batch element's the same number of rows per wave where T allows
-  const int groups = (a.T + kNormWaves - 1) / kNormWaves, cap = std::max(1, 1024 / a.B), passes = (groups + cap - 1) / cap;
+  const int groups = (int)((a.T + (long long)kNormWaves - 1) / kNormWaves), cap = std::max(1, 1024 / a.B), passes = (groups + cap - 1) / cap;
   const dim3 grid((unsigned)((groups + passes - 1) / passes), (unsigned)a.B), block(64 * kNormWaves);
   const size_t lds = (size_t)a.C * 4 * (GATE ? 3 : 2) * (TAN ? 2 : 1);
 #define TVM_NORM(N) hipLaunchKernelGGL((gate_adaln_q8_kernel<T, TAN, GATE, N>), grid, block, lds, st, a)

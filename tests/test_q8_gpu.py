@@ -521,3 +521,16 @@ def test_many_rows():
     q, s, _, _ = tvm.tvmattn_rowquant_fwd(x)
     check_rows(q[-3:], s[-3:], x[-3:].double().cpu().numpy())
     assert not q[:-3].any() and not s[:-3].any()
+
+
+def test_longest_stream():
+    """The row counter steps past the last row, and must not come back as a negative one."""
+    T, C = (1 << 31) - 1, 8                                                       # 34 GB
+    t = norm_inputs(1, 30, C, "bf16", 14)
+    x = torch.zeros(1, T, C, dtype=torch.bfloat16, device="cuda")
+    x[:, -30:] = t["x"].cuda()
+    a, b = t["a"].cuda(), t["b"].cuda()
+    _, _, q, s, _, _ = tvm.tvmattn_gate_adaln_jvp_fwd_q8(x, None, None, None, None, None, a, None, b, None, EPS)
+    _, _, rq, rs, _, _ = norm_call(t, False, False)
+    assert torch.equal(q[:, -30:], rq) and torch.equal(s[:, -30:], rs)
+    assert (q[0, :-30:9973] == q[0, 0]).all() and (s[0, :-30:9973] == s[0, 0]).all() and q[0, 0].abs().max() == 127
