@@ -448,7 +448,9 @@ int tvmattn_linear_jvp_bwd(int R, int K, int F, int dtype,
  *
  *     s = max_j |v_j| / 127,     q_j = v_j 127 / max|v| rounded to the nearest integer (ties to even)
  *
- * and stands for q s (|v_j - q_j s| <= s (1/2 + 2^-16)).  A row with nothing above 2^-100 has s = 0 and q = 0; a row that holds a
+ * and stands for q s (|v_j - q_j s| <= s (1/2 + 2^-16)).  The rounding is exact where the v_j are values that came in; where they are
+ * worked out first (the activation, the modulation) they are float32 with a few roundings of their own, and next to the border
+ * between two integers either may come out.  A row with nothing of 2^-100 or more has s = 0 and q = 0; a row that holds a
  * NaN or an infinity has s = NaN and q = 0: all that is made of it is NaN, and no other row is touched.
  * Every operator carries an optional tangent: its rows are rows like any others, with scales of their own.  Without one, the
  * tangent's pointers (inputs and outputs) are all NULL; some of them alone NULL is TVMATTN_INVALID_ARG.

@@ -2,7 +2,7 @@
 
 TEST INFRASTRUCTURE ONLY.  Imported by tests/ and nothing else; it shares no code with the HIP kernels and never calls them.
 
-A row v: s = max|v| / 127, q = v / s rounded to the nearest integer, ties to even; it stands for q s.  Zero rows have s = 0 and
+A row v: s = max|v| / 127, q = v 127 / max|v| rounded to the nearest integer, ties to even; it stands for q s.  Zero rows have s = 0 and
 q = 0; rows with a NaN or an infinity s = NaN and q = 0.  The operators whose outputs are such rows (the MLP's activation, the
 gated residual with the modulation behind it) are the other oracles' functions, then `rows8`.
 
@@ -20,7 +20,8 @@ def steps(v):
     m = np.abs(v).max(-1)
     s = np.where(np.isfinite(m), m / 127, np.nan)
     with np.errstate(divide="ignore", invalid="ignore"):
-        t = np.where((m > 0)[..., None] & np.isfinite(m)[..., None], v / s[..., None], 0.0)
+        # (not v / s, whose s is rounded: max / 2 is a tie whatever max is; 127 v is exact for float32 values)
+        t = np.where((m > 0)[..., None] & np.isfinite(m)[..., None], v * 127 / m[..., None], 0.0)
     return t, s
 
 

@@ -43,7 +43,8 @@ __device__ __forceinline__ Scale scale_of(unsigned m) {
   if (m < 0x0d800000u) return {0.f, 0.f, 0u};  // below 2^-100: 127 / top would leave float32's range
   return {top / 127.0f, 127.0f / top, ~0u};
 }
-// Four values as bytes.  v inv + 1.5 2^23 in one rounding leaves round(v inv) in the low bits (two's complement).
+// Four values as bytes.  v inv + 1.5 2^23 in one rounding leaves round(v inv) in the low bits (two's complement).  (inv is off by 2^-24,
+// like values that were worked out in float32: within 2^-16 of a step of the border between two, either may come out.)
 __device__ __forceinline__ unsigned pack4(float v0, float v1, float v2, float v3, const Scale& k) {
   constexpr float kMagic = 12582912.0f;
   const unsigned b0 = __builtin_bit_cast(unsigned, fmaf(v0, k.inv, kMagic)), b1 = __builtin_bit_cast(unsigned, fmaf(v1, k.inv, kMagic));
@@ -54,6 +55,51 @@ template <int VEC>
 __device__ __forceinline__ void store_q8(signed char* p, const float (&v)[VEC], const Scale& k) {
   if constexpr (VEC == 8) *reinterpret_cast<uint2*>(p) = make_uint2(pack4(v[0], v[1], v[2], v[3], k), pack4(v[4], v[5], v[6], v[7], k));
   else *reinterpret_cast<unsigned*>(p) = pack4(v[0], v[1], v[2], v[3], k);
+}
+// The nearest step to v 127 / top, ties to even, of values as they came in.  127 / top is not a float32, so that the product above goes to
+// either side of a tie (top / 2, 63.5 steps, is one whatever top is, and common in bf16).  Instead: with an inverse surely too
+// large and one surely too small, by 2^-22, all but one value in 60 000 come out the same, and then the exact quotient, which lies
+// strictly between, does too.  The others are next to n + 1/2 steps.
+//   bf16: v = V and top = M 2^k as integers, V and M below 2^8, k >= 0: 254 V and (2 n + 1) M 2^k are equal or 1 apart at least, 2^-16 of
+//     themselves.  So it is a tie, and of the two integers the even one is taken, byte by byte.
+//   float32: 254 v and (2 n + 1) top decide, whole numbers of at most 32 bits times one power of two, exact in float64.
+// us of one product | of this: bf16 4608 x 1152 5.9 | 5.6, 16384 x 1152 of a pitch of 3456 with tangent 19.8 | 19.4, 16384 x 2304 with
+// tangent 36.8 | 38.5; float32 with tangent 16384 x 1152 33.5 | 34.3, 4096 x 4608 38.0 | 40.8.  (bf16 by the branch into float64: 21.1 for 19.4.)
+__device__ __forceinline__ int nearest(float v, float top, int a, int b) {
+  const double x = 254.0 * (double)v, border = (double)(a + b) * (double)top;
+  return x > border ? max(a, b) : x < border ? min(a, b) : (a & 1) == 0 ? a : b;
+}
+// All of a thread's chunks of a row: w gets the bytes.
+template <typename T, int NCH>
+__device__ __forceinline__ void pack_exact(unsigned (&w)[NCH][2], const float (&v)[NCH][Chunk<T>::VEC], const Scale& k, float top) {
+  constexpr int WORDS = Chunk<T>::VEC / 4;
+  constexpr float kOff = 2.384185791015625e-07f;  // 2^-22
+  const Scale up = {k.s, k.inv * (1.0f + kOff), k.keep}, down = {k.s, k.inv * (1.0f - kOff), k.keep};
+  unsigned other[NCH][2], differ = 0;
+#pragma unroll
+  for (int j = 0; j < NCH; ++j)
+#pragma unroll
+    for (int n = 0; n < WORDS; ++n) {
+      const float* const f = v[j] + 4 * n;
+      w[j][n] = pack4(f[0], f[1], f[2], f[3], up);
+      other[j][n] = pack4(f[0], f[1], f[2], f[3], down);
+      if constexpr (sizeof(T) == 2) {
+        const unsigned odd = w[j][n] & 0x01010101u, take = (odd << 8) - odd;  // 255 in the bytes that are odd
+        w[j][n] = (w[j][n] & ~take) | (other[j][n] & take);
+      } else {
+        differ |= w[j][n] ^ other[j][n];
+      }
+    }
+  if (sizeof(T) == 4 && differ != 0) {
+#pragma unroll
+    for (int j = 0; j < NCH; ++j) {
+      unsigned exact = 0;
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        exact |= (unsigned)(nearest(v[j][e], top, (signed char)(w[j][0] >> 8 * e), (signed char)(other[j][0] >> 8 * e)) & 255) << 8 * e;
+      w[j][0] = exact;
+    }
+  }
 }
 template <int VEC>
 __device__ __forceinline__ unsigned mag_of(const float (&v)[VEC], unsigned m) {
@@ -83,6 +129,9 @@ __global__ __launch_bounds__(NW == 1 ? 256 : 64 * NW) void rows_q8_kernel(RowsQ8
     raw[0][j] = load_raw<T>(x + at);
     if constexpr (SETS == 2) raw[1][j] = load_raw<T>(tx + at);
   }
+  // All loads first: with the work below some came behind a wait for the one before (16384 x 1152 float32 with tangent 39.6 us, 34.3
+  // with the fence).  The activation's loads come first without it, and its arithmetic loses by it (43 | 45 us).
+  if constexpr (!GELU) __builtin_amdgcn_sched_barrier(0);
   float v[SETS][NCH][VEC];
   unsigned m[SETS] = {};
 #pragma unroll
@@ -119,10 +168,16 @@ __global__ __launch_bounds__(NW == 1 ? 256 : 64 * NW) void rows_q8_kernel(RowsQ8
   for (int k = 0; k < SETS; ++k) {
     const Scale sc = scale_of(m[k]);
     if (first == 0) (second || k == 1 ? a.ts : a.s)[row] = sc.s;
+    unsigned exact[NCH][2];
+    if constexpr (!GELU) pack_exact<T, NCH>(exact, v[k], sc, __builtin_bit_cast(float, m[k]));
 #pragma unroll
     for (int j = 0; j < NCH; ++j) {
       const int c = first + j * 64 * NW;
-      if (c < chunks) store_q8<VEC>(q[k] + c * VEC, v[k][j], sc);
+      if (c >= chunks) continue;
+      signed char* const p = q[k] + c * VEC;
+      if constexpr (GELU) store_q8<VEC>(p, v[k][j], sc);
+      else if constexpr (VEC == 8) *reinterpret_cast<uint2*>(p) = make_uint2(exact[j][0], exact[j][1]);
+      else *reinterpret_cast<unsigned*>(p) = exact[j][0];
     }
   }
 }
