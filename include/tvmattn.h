@@ -466,7 +466,8 @@ int tvmattn_rowquant_fwd(int R, int C, int dtype, const void* x, const void* tx,
 
 /*
  * The MLP's activation (tvmattn_gelu_jvp_fwd: a = gelu(u), ta = gelu'(u) tu) with its outputs as 8-bit rows; a and ta are not
- * rounded in between.  Arguments and limits as above.
+ * rounded in between.  gelu and gelu' are float32 values right to 2^-16 of their size, however small (gelu' next to its zero at
+ * u = -0.752: to 2^-22; below 2^-118, u < -10, it counts as 0).  Arguments and limits as above.
  */
 int tvmattn_gelu_jvp_fwd_q8(int R, int C, int dtype, const void* u, const void* tu, long long ldu,
                             void* q, float* s, void* tq, float* ts, void* hip_stream);

@@ -28,5 +28,23 @@ __device__ __forceinline__ Gelu gelu_parts(float u) {
   return g;
 }
 
+// gelu and gelu' to a few float32 roundings of their own size, also where they are tiny (u at -9: 2^-93): what an 8-bit row needs, whose
+// step is its largest value's.  (Above, 1 - r for r near 1 has an error of 2^-24 whatever its size; rows around u = -4.5 came out 4 steps
+// off and rows around -6 lost.)  (1 + tanh w)/2 =: s = 1/(1 + exp(-2w)), a sum of positive numbers, is 0 or 1 where exp leaves the range;
+// gelu = u s,  gelu' = s + 2 u w' (s - s^2): the difference is as good as s for u < 0, and for u > 0, where s is near 1, off by 2^-24 of
+// gelu' times 2 u w' (35 at u = 5; behind that s is 1).
+struct GeluSmall {
+  float s, g1;
+};
+template <bool FIRST>
+__device__ __forceinline__ GeluSmall gelu_small(float u) {
+  constexpr double kW = 0.79788456080286535588, kL = -2.0 * kW * 1.44269504088896340736;  // -2 w log2 e = kL (u + c u^3)
+  const float u2 = u * u;
+  GeluSmall g;
+  g.s = __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(u * fmaf((float)(kL * 0.044715), u2, (float)kL)));
+  g.g1 = FIRST ? fmaf(u, fmaf((float)(6.0 * kW * 0.044715), u2, (float)(2.0 * kW)) * fmaf(-g.s, g.s, g.s), g.s) : 0.f;
+  return g;
+}
+
 }  // namespace
 }  // namespace tvm
