@@ -32,7 +32,8 @@ __device__ __forceinline__ Gelu gelu_parts(float u) {
 // step is its largest value's.  (Above, 1 - r for r near 1 has an error of 2^-24 whatever its size; rows around u = -4.5 came out 4 steps
 // off and rows around -6 lost.)  (1 + tanh w)/2 =: s = 1/(1 + exp(-2w)), a sum of positive numbers, is 0 or 1 where exp leaves the range;
 // gelu = u s,  gelu' = s + 2 u w' (s - s^2): the difference is as good as s for u < 0, and for u > 0, where s is near 1, off by 2^-24 of
-// gelu' times 2 u w' (35 at u = 5; behind that s is 1).
+// gelu' times 2 u w' (35 at u = 5; behind that s is 1).  From |u| = 16 on s is 0 or 1, s - s^2 is 0, and w' is
+// taken at 16: no finite u makes an infinity there to multiply with 0.
 struct GeluSmall {
   float s, g1;
 };
@@ -42,7 +43,7 @@ __device__ __forceinline__ GeluSmall gelu_small(float u) {
   const float u2 = u * u;
   GeluSmall g;
   g.s = __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(u * fmaf((float)(kL * 0.044715), u2, (float)kL)));
-  g.g1 = FIRST ? fmaf(u, fmaf((float)(6.0 * kW * 0.044715), u2, (float)(2.0 * kW)) * fmaf(-g.s, g.s, g.s), g.s) : 0.f;
+  g.g1 = FIRST ? fmaf(u, fmaf((float)(6.0 * kW * 0.044715), fminf(u2, 256.0f), (float)(2.0 * kW)) * fmaf(-g.s, g.s, g.s), g.s) : 0.f;
   return g;
 }
 

@@ -1,4 +1,4 @@
-"""The activation into 8-bit rows where u is far from zero: rows whose largest value is tiny.
+"""The activation into 8-bit rows where u is far from zero: rows whose largest value is tiny, and values whose square leaves float32.
 
 Reference in float64 with the activation as u s, s = t / (1 + t) or 1 / (1 + t) from t = exp(-2|w|), w = sqrt(2/pi) (u + 0.044715 u^3):
 no difference of numbers near 1, so that its relative error stays at 2^-45 down to exp's underflow.  (0.5 u (1 + tanh w) in float64
@@ -56,6 +56,19 @@ def test_tangents_that_live_at_negative_values_only(dtype):
     tu.zero_()
     u[:, 17:1152:38], tu[:, 17:1152:38] = far, tfar
     a, ta = reference(wl.to_f64(u), wl.to_f64(tu))
+    q, s, tq, ts = tvm.tvmattn_gelu_jvp_fwd_q8(u.cuda(), tu.cuda())
+    check_rows(q, s, a)
+    check_rows(tq, ts, ta)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("value", [1e13, 1e20, 3e38, -1e13, -1e20, -3e38])
+def test_values_whose_powers_leave_float32(value, dtype):
+    """The activation is u or 0 there and its derivative 1 or 0: the row's other tangents stay what they are."""
+    u, tu = rows(5, 3, 1152, 0.0, 2.0, dtype)
+    u[1, 700] = value
+    a, ta = reference(wl.to_f64(u), wl.to_f64(tu))
+    assert np.isfinite(a).all() and np.isfinite(ta).all()
     q, s, tq, ts = tvm.tvmattn_gelu_jvp_fwd_q8(u.cuda(), tu.cuda())
     check_rows(q, s, a)
     check_rows(tq, ts, ta)
