@@ -416,12 +416,19 @@ def tvmattn_jvp_bwd_qknorm(q, tq, k, tk, gain_q, gain_k, eps, qn, tqn, kn, tkn, 
     return out
 
 
+def _int32(*sizes):
+    """Sizes as the library's 32-bit arguments take them (ctypes would pass others modulo 2^32)."""
+    if max(sizes) >= 1 << 31:
+        raise ValueError(f"sizes of 2^31 and above are not supported: {sizes}")
+    return sizes
+
+
 def _adaln_args(x, tx, mods):
     if x.dim() != 3 or not x.is_contiguous() or not x.is_cuda:
         raise ValueError("expected contiguous [B,T,C] device tensors")
     if tx.shape != x.shape or tx.dtype != x.dtype or not tx.is_contiguous():
         raise ValueError("x and its tangent must agree in shape, dtype and layout")
-    B, T, C = x.shape
+    B, T, C = _int32(*x.shape)
     for m in mods:
         if m.shape != (B, C) or m.dtype != torch.float32 or not m.is_contiguous() or m.device != x.device:
             raise ValueError("scale, shift and their tangents must be contiguous float32 [B,C] tensors")
@@ -555,9 +562,9 @@ def _rows(t, cols, what):
     if not t.is_cuda or t.shape[-1] != cols or t.stride(-1) != 1:
         raise ValueError(f"{what}: expected device tensors [..., {cols}] with unit inner stride")
     if t.is_contiguous():
-        return t.numel() // cols, cols
+        return _int32(t.numel() // cols, cols)
     if t.dim() == 2:
-        return t.shape[0], t.stride(0)
+        return _int32(t.shape[0], cols)[0], t.stride(0)
     raise ValueError(f"{what}: a non-contiguous tensor must be given as a 2-D [R, {cols}] view")
 
 
@@ -751,7 +758,7 @@ def tvmattn_linear_jvp_fwd_q8(xq, xs, txq, txs, wq, ws, bias=None, dtype=torch.b
             return _taken(r)
     if wq.dim() != 2 or wq.dtype != torch.int8 or not wq.is_contiguous() or wq.device != xq.device:
         raise ValueError("the weight must be a contiguous int8 [F, K] tensor on the rows' device")
-    F, K = wq.shape
+    F, K = _int32(*wq.shape)
     if ws.shape != (F,) or ws.dtype != torch.float32 or not ws.is_contiguous() or ws.device != xq.device:
         raise ValueError("the weight's scales must be a contiguous float32 [F] tensor on its device")
     if xq.dtype != torch.int8 or xq.dim() < 1:
