@@ -1,6 +1,7 @@
 // The block's linear layers on 8-bit rows (gfx950): y = (xq wq^T) o (xs ws^T) + b, ty = (txq wq^T) o (txs ws^T), with a float32 scale
 // for each token row and each output channel (q8.h).  The products are exact: 8-bit integers into 32-bit sums, which K <= 2^16 keeps
-// in range; one rounding takes the sum to float32, and one the result to its type.
+// in range.  A sum is rounded to float32 (from 2^24 on), times its row's scale, and once more with its channel's scale and the bias (fused);
+// a bf16 result is then rounded to its type.
 //
 // A 16-byte fragment holds 16 entries of a row where bf16 has 8, and one 32 x 32 x 32 product takes the cycles of a 32 x 32 x 16 one in
 // bf16: tiles of 128 bytes x N rows lie in LDS as they do there (Operand, linear_gemm.h, with two entries to its one), and a
@@ -165,7 +166,8 @@ __global__ __launch_bounds__(256, OCC) void linear_q8_kernel(LinearQ8Args g, Til
 #pragma unroll
     for (int b = 0; b < W; ++b)
 #pragma unroll
-      for (int r = 0; r < 16; ++r) out[b][r] = fmaf((float)acc[a][b][r] * xs[a], ws[b][r >> 2][r & 3], bf[b][r >> 2][r & 3]);
+      for (int r = 0; r < 16; ++r)
+        out[b][r] = fmaf((float)acc[a][b][r] * (xs[a] * kRowShift), ws[b][r >> 2][r & 3] * kChannelShift, bf[b][r >> 2][r & 3]);
     if constexpr (sizeof(T) == 2) {
       store_tile_coalesced<W>(lw, y + jw, g.ldy, i0 + (wi * W + a) * 32, g.R, g.F - jw, out, 1.f, lane);
     } else if (i < g.R) {

@@ -61,7 +61,7 @@ __global__ __launch_bounds__(64 * NW) void linear_q8_few_kernel(LinearQ8Args g, 
   const f32x4 b4 = bias.values();
   f32x4 o;
 #pragma unroll
-  for (int e = 0; e < 4; ++e) o[e] = fmaf((float)acc[e] * xs, ws[e], b4[e]);
+  for (int e = 0; e < 4; ++e) o[e] = fmaf((float)acc[e] * (xs * kRowShift), ws[e] * kChannelShift, b4[e]);
   store_four(static_cast<T*>(first ? g.y[0] : g.y[1]) + (long long)r * g.ldy + f, o);
 }
 

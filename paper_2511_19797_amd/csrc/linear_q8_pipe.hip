@@ -234,10 +234,10 @@ __global__ __launch_bounds__(256, 1) void q8_pipe_kernel(LinearQ8Args g, TileOrd
     const unsigned sc = ldss + par * kScales, column = (unsigned)(wj * (WJ * 32) + 8 * ((lane & 15) >> 2) + 4 * hh + (lane & 3));
     float xs[kWI], ws[WJ], bias[WJ];
 #pragma unroll
-    for (int a = 0; a < kWI; ++a) xs[a] = *(fp)(uintptr_t)(sc + (unsigned)((wi * kWI + a) * 32 + ic) * 4u);
+    for (int a = 0; a < kWI; ++a) xs[a] = *(fp)(uintptr_t)(sc + (unsigned)((wi * kWI + a) * 32 + ic) * 4u) * kRowShift;
 #pragma unroll
     for (int b = 0; b < WJ; ++b) {
-      ws[b] = *(fp)(uintptr_t)(sc + 1024u + (column + b * 32) * 4u);
+      ws[b] = *(fp)(uintptr_t)(sc + 1024u + (column + b * 32) * 4u) * kChannelShift;
       if constexpr (WIDE) bias[b] = *(fp)(uintptr_t)(sc + 2048u + (column + b * 32) * 4u);
       else bias[b] = __builtin_bit_cast(float, (unsigned)*(sp)(uintptr_t)(sc + 2048u + (column + b * 32) * 2u) << 16);
     }
