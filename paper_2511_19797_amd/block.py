@@ -65,8 +65,13 @@ def block_q8_params(params):
 
 
 def block_jvp_fwd_q8(x, tx, mods, tmods, q8_params, H, eps, qk_eps):
-    """block_jvp_fwd where no gradient will be taken (sampling, the target network of the loss), its linear layers in 8 bits: every
-    operand of theirs leaves the operator before it as 8-bit rows.  q8_params: from block_q8_params.  Returns (z, tz)."""
+    """block_jvp_fwd where no gradient will be taken, its linear layers in 8 bits: every operand of theirs leaves the operator before it
+    as 8-bit rows.  Arguments as block_jvp_fwd's, bf16; q8_params: from block_q8_params.  The tangent is needed: the QK-norm and the
+    attention in between take no call without one (the 8-bit operators do, one by one).  Returns (z, tz)."""
+    if tx is None or tmods is None:
+        raise ValueError("the block's forward carries a tangent: its QK-norm and attention take no call without one")
+    if x.dtype != torch.bfloat16:
+        raise ValueError(f"the block's forward in 8 bits is bfloat16, not {x.dtype}")
     B, T, C = x.shape
     d = C // H
     p = q8_params
