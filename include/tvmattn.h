@@ -483,6 +483,7 @@ int tvmattn_gelu_jvp_fwd_q8(int R, int C, int dtype, const void* u, const void* 
  *                                tx itself
  *        q, tq [B*T,C] int8;  s, ts [B*T] float32
  * h NULL: no residual; c, th, tc, z and tz are NULL too, and y is the modulation of x (a block's entry).
+ * The sums of squares are float32 like the rest: z, a, b and c up to 2^63 / sqrt(C) (tvmattn_adaln_jvp_fwd has the same limit).
  * C must be a multiple of 16 bytes' worth of elements and at most 512 such chunks, B at most 65535; otherwise
  * TVMATTN_UNSUPPORTED.  One launch, no workspace.  Arithmetic is float32.
  */

@@ -6,7 +6,7 @@ A row v: s = max|v| / 127, q = v 127 / max|v| rounded to the nearest integer, ti
 q = 0; rows with a NaN or an infinity s = NaN and q = 0.  The operators whose outputs are such rows (the MLP's activation, the
 gated residual with the modulation behind it) are the other oracles' functions, then `rows8`.
 
-Pins (tests/test_q8_oracle.py): scalar loops, the largest error of a step's half, rows whose values are whole steps, ties, zero
+Pins (tests/test_q8_oracle.py, tests/test_q8_ties_oracle.py): scalar loops, the largest error of a step's half, rows whose values are whole steps, ties, zero
 rows, non-finite rows; the linear layer against its definition in Python integers.
 """
 import numpy as np

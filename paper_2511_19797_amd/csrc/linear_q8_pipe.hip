@@ -8,11 +8,11 @@
 // as row broadcasts (a data-parallel-primitive operand): two registers per block instead of 32.  They come by asynchronous loads
 // into LDS, asked for when the output tile begins: with loads into registers the compiler waited, at the tile's end, for every
 // load in flight.
-// us (POP/s) on 256 x 192, bf16 results: 2 x 16384 x 1152 -> 3456 146 (1.8), -> 1152 52 (1.7), -> 4608 188 (1.85), 2 x 16384 x 4608 -> 1152
+// us (POP/s) on 256 x 192, bf16 results, on one card (by card the first takes 140 to 165): 2 x 16384 x 1152 -> 3456 146 (1.8), -> 1152 52 (1.7), -> 4608 188 (1.85), 2 x 16384 x 4608 -> 1152
 // 145 (2.4), 8192 x 4608 -> 1152 42 (2.1); float32 results, 1152 -> 3456 162; on 128 x 128 tiles 213, 76, 293, 213, 67; 260.  What bounds it is
-// power: at 2.4 POP/s the clock is 1.75 GHz with the matrix cores 64 % busy, and changes that save cycles (the barrier's slot, the
-// order of fragment reads, of tiles) leave the times as they are.  At K = 1152 an output tile's end is a third of its cycles, 12 k of 30 k;
-// 256 x 256 tiles are no faster there (146 against 144 at -> 3456) and lose where they do not divide the layer (167 against 148
+// power at K = 4608: at 2.4 POP/s the clock is 1.75 GHz with the matrix cores 64 % busy, and changes that save cycles (the barrier's slot,
+// the order of fragment reads, of tiles) leave the times as they are.  At K = 1152 the clock is 1.97 GHz and they are 47 % busy: an output
+// tile's end is a third of its cycles, 12 k of 30 k, and what hides it costs as much in LDS traffic.  256 x 256 tiles are no faster there (146 against 144 at -> 3456) and lose where they do not divide the layer (167 against 148
 // at 4608 -> 1152).  256 x 128 is for shapes whose tiles it deals out better: 2 x 1000 x 1152 -> 3456 12.1 us, 14.4 on 256 x 192.
 #include <type_traits>
 

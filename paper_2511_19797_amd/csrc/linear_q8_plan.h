@@ -17,8 +17,8 @@ inline long long tiles_q8(int n, int R, int F) {
 inline bool grid_fits_q8(int n, long long tiles) { return n <= kQ256x128 || small_workgroups(tiles) * kSmallThreads < (1ll << 32); }
 // Tile shape of `sets` products [R][K] x [F][K]: the model of product_ns (linear_plan.h), with contraction tiles of 128.  The weights are
 // fits to times of all four shapes at 1100 products of R = 9 ... 16384 rows, K = 64 ... 4608 and F = 64 ... 6912, one and two sets,
-// bf16 and float32 results; the choice is 0.05 % behind the fastest shape on average and 7.7 % at most.  Some of the times, back to
-// back (us; 256 x 192 | 256 x 128 | 128 | 64):
+// bf16 and float32 results; the choice is 0.05 % behind the fastest shape on average and 7.7 % at most, and more than 1 % at 14 of them
+// (always 64 x 64: 10 % on average, 256 x 192: 106 %).  Some of the times, back to back (us; 256 x 192 | 256 x 128 | 128 | 64):
 //   2 x 256 x 1152 -> 1152:    14.0 | 11.1 |  8.9 | 5.7    few tiles: small ones fill the chip
 //   512 x 1152 -> 4608:        14.1 | 11.5 |  9.7 | 10.0   one round of 128, two of 64
 //   2 x 1000 x 1152 -> 3456:   14.4 | 12.1 | 16.7 | 19.0   216 tiles of 256 x 128, one round of 256 workgroups, against 144 of 192

@@ -5,8 +5,9 @@
 //
 // A row belongs to one wave where it fits (4 chunks of 16 bytes per lane: 2048 bf16 values), so that its maximum and its sums
 // are lane exchanges, with no barrier; longer rows belong to 4 or 16 waves, which meet once in LDS.
-// us (TB/s of what has to be read and written): rows of 16384 x 1152 with tangent, bf16, 19.6 (5.8); activation 16384 x 4608 with tangent 76.7
-// (5.9), 250 x 1536 float32 2.7; norm with residual and tangent 16 x 1024 x 1152 50.5 (5.2), 1 x 256 x 1152 6.4.
+// us (TB/s of what has to be read and written): rows of 16384 x 1152 with tangent, bf16, 19.6 (5.8), float32 34.8 (5.4); activation 16384 x
+// 4608 with tangent 77 (5.9), without 41 (5.5), 250 x 1536 float32 2.7; norm with residual 16 x 1024 x 1152 with tangent 50.4 (5.2), without
+// 24.5 (5.4), float32 with tangent 99 (5.0), 1 x 256 x 1152 6.4.
 #include <algorithm>
 
 #include "gelu_math.h"
@@ -189,6 +190,8 @@ __global__ __launch_bounds__(NW == 1 ? 256 : 64 * NW) __attribute__((amdgpu_wave
 // into LDS (with the tangents 24 bytes per column), and its four waves then take a row each, with no further barrier.  120 registers
 // at three chunks per lane, four waves per SIMD: with a row's chunks interleaved and the next row's on their way it took 256, and 71 us
 // instead of 50 at 16 x 1024 x 1152.
+// From 5 to 8 chunks per lane there is one instance, at one wave per SIMD: 4 x 1024 x 2048 with tangent 23.9 us, x 2056 45.5, x 4096 72;
+// without 12.3 and 15.6.
 constexpr int kNormWaves = 4;  // (2 | 4 | 8: 16 x 1024 x 1152 118 | 50 | 52 us, 1 x 256 x 1152 8.3 | 6.4 | 7.2)
 template <typename T, bool TAN, bool GATE, int NCH>
 __global__ __launch_bounds__(64 * kNormWaves, NCH <= 3 ? 4 : NCH == 4 ? 3 : 1) void gate_adaln_q8_kernel(GateAdalnQ8Args g) {
