@@ -503,8 +503,9 @@ int tvmattn_gate_adaln_jvp_fwd_q8(int B, int T, int C, int dtype,
  *        bias      [F] dtype, or NULL
  *   out: y, ty     [R,F] dtype (float32 or bfloat16), rows ldy elements apart (0 = F: dense)
  * The sums are exact (32-bit integers).  A result has three roundings in float32 (the sum from 2^24 on, times its row's scale, with its
- * channel's scale and the bias) and one to bfloat16 if that is its type; none of its parts leaves float32 where it does not, for any
- * finite xs and for ws below 2^104.  K and ldx must be multiples of 16, F and
+ * channel's scale and the bias) and one to bfloat16 if that is its type; none of its parts leaves float32 where it does not, for xs
+ * below 2^122 (all that rows of finite values have) and ws below 2^104.  (xs below 2^-102, rows with nothing of 2^-95: the second
+ * rounding is one of a denormal number, up to 2^-18.)  K and ldx must be multiples of 16, F and
  * ldy of 8, K at most 2^16, F and the pitches at most 2^20, R at most 2^30, R F at most 2^38; otherwise TVMATTN_UNSUPPORTED.  One launch, no workspace.
  */
 int tvmattn_linear_jvp_fwd_q8(int R, int K, int F, int dtype, const void* xq, const float* xs, const void* txq,

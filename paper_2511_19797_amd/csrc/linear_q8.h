@@ -17,8 +17,8 @@ __device__ __forceinline__ int lane_chunk(int wave, int lane) {
 }
 
 // A result is fma(fl(fl(sum) xs), ws, bias): three roundings in float32, a fourth to bf16.  The sum (below 2^30) times a token's scale may
-// leave float32's range where the result does not, so the scales are taken as xs 2^-24 and ws 2^24: the same bits, for every finite xs
-// and for ws below 2^104.
+// leave float32's range where the result does not, so the scales are taken as xs 2^-24 and ws 2^24: the same bits for xs from 2^-102 (below,
+// xs 2^-24 is denormal and loses up to five of its bits) to 2^122 (max / 127 is smaller) and for ws below 2^104.
 constexpr float kRowShift = 5.9604644775390625e-08f, kChannelShift = 16777216.0f;
 
 // Four consecutive floats or bf16 values: loaded as they are, bounds-checked (zeros beyond), and as floats.
