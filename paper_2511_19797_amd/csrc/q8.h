@@ -1,8 +1,8 @@
 // The 8-bit operators around the block's linear layers (rows_q8.hip, linear_q8.hip): arguments and launchers.
 //
 // An 8-bit row: s = max|v| / 127 in float32 and q_j = round(v_j 127 / max|v|) to the nearest integer, ties to even; it stands for
-// q s.  Exactly so for values that came in; values that are worked out first are float32 with roundings of their own, and within
-// 2^-16 of a step of the border between two integers either may come out.  A row of zeros (or with nothing of 2^-100 or more) has
+// q s.  Exactly so for values that came in; values that are worked out first are float32 with a few roundings of their own, and next to
+// the border between two integers either may come out (the rounding itself is off by 2^-17 of a step at most).  A row of zeros (or with nothing of 2^-100 or more) has
 // s = 0 and q = 0; one that holds a NaN or an infinity has s = NaN and q = 0, so that whatever is made of it is NaN.
 #pragma once
 #include "tvm_common.h"

@@ -44,8 +44,8 @@ __device__ __forceinline__ Scale scale_of(unsigned m) {
   if (m < 0x0d800000u) return {0.f, 0.f, 0u};  // below 2^-100: 127 / top would leave float32's range
   return {top / 127.0f, 127.0f / top, ~0u};
 }
-// Four values as bytes.  v inv + 1.5 2^23 in one rounding leaves round(v inv) in the low bits (two's complement).  (inv is off by 2^-24,
-// like values that were worked out in float32: within 2^-16 of a step of the border between two, either may come out.)
+// Four values as bytes.  v inv + 1.5 2^23 in one rounding leaves round(v inv) in the low bits (two's complement).  (inv is off by 2^-24:
+// for values that were worked out in float32 and are off by as much.)
 __device__ __forceinline__ unsigned pack4(float v0, float v1, float v2, float v3, const Scale& k) {
   constexpr float kMagic = 12582912.0f;
   const unsigned b0 = __builtin_bit_cast(unsigned, fmaf(v0, k.inv, kMagic)), b1 = __builtin_bit_cast(unsigned, fmaf(v1, k.inv, kMagic));
